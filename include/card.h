@@ -460,6 +460,100 @@ int card_step_begin_sampled(card_cache* cache, const card_model_cfg* cfg, const 
 int card_step_end(card_cache* cache, const card_step* step_host, const card_verify_result* out_host,
                   int32_t flags, int32_t* emitted_host, int32_t* n_emitted_host);
 
+/* ------------------------------------------------------------------------------------------
+ * Several sequences on one pair of page pools.  The pools are as card_kv has them (same pages, same
+ * order inside them, so steps, prompts and drafts above run on a sequence of such a pool through its
+ * row of the block tables); which pages a sequence has is the caller's bookkeeping.  Of cfg these functions take the
+ * layers, the heads and the head size.
+ *
+ * card_kv_copy_pages: page dst_host[i] becomes a copy of page src_host[i], in both pools and all layers.
+ * A fork of a sequence shares its full pages and copies the one that both go on writing.  CARD_ERANGE: a
+ * page outside [0, n_pages); CARD_EINVAL: a page is written twice, or is both read and written.
+ *
+ * card_kv_move_slots: slot dst_host[i] becomes a copy of slot src_host[i], in both pools and all layers; slot
+ * page * 16 + t is place t of a page.  Accepted nodes of a draft's tree move to where the text continues; a
+ * sequence that gives up tokens closes the gaps.  The moves act as if one after the other; CARD_EINVAL: a
+ * slot is written twice, or read after an earlier move wrote it (closing gaps from the front never does).
+ * CARD_ERANGE: a slot outside the pool.  Slots beside the written ones keep what they hold: a
+ * page that nothing was ever written to has to be cleared before a step or a prompt reads it.
+ *
+ * The lists are host memory, read during the call only (they travel with the launches, also into a
+ * captured graph); kv->block_table and pending_token are not used. */
+int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host,
+                       const int32_t* dst_host, void* stream);
+int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host,
+                       const int32_t* dst_host, void* stream);
+
+/* A ragged batch: sequence s has ctx_lens[s] tokens in the cache and the new tokens of rows row_starts[s] ..
+ * row_starts[s + 1] - 1, at the positions behind them.  What lies in device memory may change between
+ * the replays of a captured graph. */
+typedef struct card_kv_batch {
+    void* k_pages; /* dev, as in card_kv                                                         */
+    void* v_pages;
+    int32_t n_pages;
+    int32_t n_seqs;
+    const int32_t* block_tables; /* dev [n_seqs][table_pages], entries in [0, n_pages) as far as the sequence reaches */
+    int32_t table_pages;
+    int32_t n_rows;            /* rows of the arrays of the call                                 */
+    const int32_t* ctx_lens;   /* dev [n_seqs]                                                   */
+    const int32_t* row_starts; /* dev [n_seqs + 1], ascending from 0, the last one at most n_rows */
+    int32_t max_new;           /* most new tokens, and most tokens in all, of one sequence: how the work is cut goes */
+    int32_t max_len;           /* by them (0: not known); results are right whatever they say    */
+} card_kv_batch;
+
+/* Rows of heads: element j of head a of row i at data[i * row_stride + a * head_stride + j], strides in elements. */
+typedef enum card_type { CARD_BF16 = 0, CARD_F32 = 1 } card_type;
+typedef struct card_rows {
+    void* data; /* dev */
+    int32_t type;
+    int64_t row_stride, head_stride;
+} card_rows;
+
+/* What a row sees instead of all tokens up to its own: every slot of its sequence below mask_base[s], and
+ * slot mask_base[s] + j iff bit j % 32 of mask[row * words + j / 32] is set (as card_tree_rows says it). */
+typedef struct card_row_mask {
+    const uint32_t* mask_dev;     /* [n_rows][words]  */
+    const int32_t* mask_base_dev; /* [n_seqs], >= 0   */
+    int32_t words;
+} card_row_mask;
+
+/* Attention of the new tokens over the cache, one layer: stores their keys and values (rotated as the caller wants them,
+ * rounded to bf16) behind what their sequences hold, then out = softmax(q k / sqrt(head_dim)) v for each new row and query head over the
+ * tokens of its sequence up to its own, or over what `mask` lets it see.  A row that sees nothing is zero.
+ *   q, out  : n_q_heads heads; k, v: n_kv_heads heads, or both NULL where the cache holds the new tokens already.  All of one
+ *             type: CARD_BF16, or CARD_F32, whose products keep 32-bit accuracy.  Data and strides in multiples of 16 bytes;
+ *             strides of out at least head_dim; out overlaps no other array.  Rows behind row_starts[n_seqs] are not touched.
+ *   mask    : NULL = causal
+ *   workspace_dev : card_kv_attend_workspace_bytes, 16-byte aligned (NULL where that is 0), no preparation; calls that may run
+ *             at the same time do not share one
+ * Stored values are taken to be finite, also those that a mask hides; what the slots behind a sequence's end hold does not
+ * matter here and is kept (a pool that steps and prompts run on too is cleared once before its first use: they take every slot of
+ * a page that they read as finite).  Device data that is out of its range reads and writes nothing outside the buffers: tokens whose page
+ * is outside the pool or the table are not stored and not seen.
+ * The sums of a row are taken in an order that depends on the sizes of the call (n_rows, n_seqs, max_new, max_len) and
+ * on its sequence, not on what runs beside it: the same call gives the same bits.
+ * Errors: CARD_EINVAL, CARD_ERANGE (layer; n_rows * n_q_heads >= 2^31), CARD_EDEVICE; nothing is enqueued on error. */
+size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch);
+int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q,
+                   const card_rows* k, const card_rows* v, const card_rows* out, const card_row_mask* mask,
+                   void* workspace_dev, void* stream);
+
+/* Log probabilities of given tokens, with the entropy and the most probable tokens of their distributions, p = softmax(logits / temperature).
+ *   logits_dev : [rows][vocab], CARD_F32 or CARD_BF16, row_stride elements apart (>= vocab)
+ *   tokens_dev : int32 [rows], or NULL; logprob_dev: fp32 [rows] (with tokens_dev): ln p of the token; 0 where the token is
+ *                negative (no token), NaN where it is not below vocab
+ *   entropy_dev: fp32 [rows] or NULL: -sum p ln p
+ *   top        : 0..32; top_tokens_dev int32 / top_logprobs_dev fp32 [rows][top], most probable first, equal logits by
+ *                ascending token id; token -1 and -inf where fewer tokens than that have a logit above -inf
+ *   workspace_dev: card_logprobs_workspace_bytes, 16-byte aligned, no preparation; calls that may run at the same time do not share one
+ * A logit of -inf is a token without probability (its log probability is -inf).  A row in which no logit is above -inf has log
+ * probabilities of -inf and entropy 0; a row with a NaN or +inf is void: NaN, and tokens -1.
+ * Errors: CARD_EINVAL, CARD_ERANGE (top), CARD_EDEVICE. */
+size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
+int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride,
+                  const int32_t* tokens_dev, float temperature, int32_t top, float* logprob_dev, float* entropy_dev,
+                  int32_t* top_tokens_dev, float* top_logprobs_dev, void* workspace_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

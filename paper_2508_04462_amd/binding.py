@@ -11,6 +11,7 @@ lib_path = os.path.join(_PKG, "libcard.so")
 CARD_OK, CARD_EINVAL, CARD_ERANGE, CARD_ECAPACITY, CARD_EDEVICE, CARD_ESTALE, CARD_ETOOBIG = 0, -1, -2, -3, -4, -5, -6
 
 CARD_CODED = 1 << 30  # in the header's grid_wgs
+CARD_BF16, CARD_F32 = 0, 1
 
 TENSOR_IDS = {
     "embed": 0, "wq": 1, "wk": 2, "wv": 3, "wo": 4, "wg": 5, "wu": 6, "wd": 7,
@@ -55,6 +56,22 @@ class CardKV(C.Structure):
         ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("block_table", C.c_void_p),
         ("n_pages", C.c_int32), ("pending_token", C.c_int32),
     ]
+
+
+class CardKVBatch(C.Structure):
+    _fields_ = [
+        ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("n_pages", C.c_int32), ("n_seqs", C.c_int32),
+        ("block_tables", C.c_void_p), ("table_pages", C.c_int32), ("n_rows", C.c_int32),
+        ("ctx_lens", C.c_void_p), ("row_starts", C.c_void_p), ("max_new", C.c_int32), ("max_len", C.c_int32),
+    ]
+
+
+class CardRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("type", C.c_int32), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class CardRowMask(C.Structure):
+    _fields_ = [("mask_dev", C.c_void_p), ("mask_base_dev", C.c_void_p), ("words", C.c_int32)]
 
 
 class CardSampling(C.Structure):
@@ -148,6 +165,18 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.card_verify_debug_logits.argtypes = [_cfgp, _P, _kvp, C.c_int32, _P, C.c_int32, _P, _P, _P, _P, _P]
     lib.card_kv_gather.restype = C.c_int
     lib.card_kv_gather.argtypes = [_cfgp, _kvp, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]
+    for _n in ("card_kv_copy_pages", "card_kv_move_slots"):
+        getattr(lib, _n).restype = C.c_int
+        getattr(lib, _n).argtypes = [_cfgp, _kvp, C.c_int32, _i32p, _i32p, _P]
+    _rowsp = C.POINTER(CardRows)
+    lib.card_kv_attend_workspace_bytes.restype = C.c_size_t
+    lib.card_kv_attend_workspace_bytes.argtypes = [_cfgp, C.POINTER(CardKVBatch)]
+    lib.card_kv_attend.restype = C.c_int
+    lib.card_kv_attend.argtypes = [_cfgp, C.POINTER(CardKVBatch), C.c_int32, _rowsp, _rowsp, _rowsp, _rowsp, C.POINTER(CardRowMask), _P, _P]
+    lib.card_logprobs_workspace_bytes.restype = C.c_size_t
+    lib.card_logprobs_workspace_bytes.argtypes = [C.c_int32] * 3
+    lib.card_logprobs.restype = C.c_int
+    lib.card_logprobs.argtypes = [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_float, C.c_int32] + [_P] * 6
     lib.card_profile_enable.restype = C.c_int
     lib.card_profile_enable.argtypes = [C.c_int32]
     lib.card_profile_disable.restype = C.c_int
@@ -339,6 +368,61 @@ def card_kv_gather(cfg, kv: CardKV, layer: int, first_slot: int, count: int, k_o
                               _ptr(v_out_dev), _ptr(stream))
 
 
+def card_kv_copy_pages(cfg, kv: CardKV, src_pages, dst_pages, stream=None) -> int:
+    if len(src_pages) != len(dst_pages):
+        return CARD_EINVAL
+    return lib.card_kv_copy_pages(C.byref(cfg), C.byref(kv), len(src_pages), _i32(src_pages), _i32(dst_pages), _ptr(stream))
+
+
+def card_kv_move_slots(cfg, kv: CardKV, src_slots, dst_slots, stream=None) -> int:
+    if len(src_slots) != len(dst_slots):
+        return CARD_EINVAL
+    return lib.card_kv_move_slots(C.byref(cfg), C.byref(kv), len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
+
+
+_TYPES = {"torch.bfloat16": CARD_BF16, "torch.float32": CARD_F32}
+
+
+def _type(t) -> int:
+    """A tensor's card_type; -1, which every entry point refuses, for types that there are none for."""
+    return _TYPES.get(str(t.dtype), -1)
+
+
+def card_rows(t) -> CardRows:
+    """A tensor [rows][heads][head_dim] as card_kv_attend takes it; its last dimension has to be contiguous."""
+    rows, heads, h = t.shape
+    if t.stride(2) != 1:
+        raise ValueError("the elements of a head have to lie side by side")
+    # (the stride of a dimension of one says nothing)
+    return CardRows(t.data_ptr(), _type(t), t.stride(0) if rows > 1 else heads * h, t.stride(1) if heads > 1 else h)
+
+
+def card_kv_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:
+    return lib.card_kv_attend_workspace_bytes(C.byref(cfg), C.byref(batch))
+
+
+def card_kv_attend(cfg, batch: CardKVBatch, layer: int, q: CardRows, k: Optional[CardRows], v: Optional[CardRows], out: CardRows,
+                   mask: Optional[CardRowMask], workspace_dev, stream=None) -> int:
+    return lib.card_kv_attend(C.byref(cfg), C.byref(batch), layer, C.byref(q), None if k is None else C.byref(k),
+                              None if v is None else C.byref(v), C.byref(out), None if mask is None else C.byref(mask),
+                              _ptr(workspace_dev), _ptr(stream))
+
+
+def card_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    return lib.card_logprobs_workspace_bytes(rows, vocab, top)
+
+
+def card_logprobs(logits, tokens_dev, temperature: float, top: int, logprob_dev, entropy_dev, top_tokens_dev, top_logprobs_dev,
+                  workspace_dev, stream=None) -> int:
+    """logits: a tensor [rows][vocab] whose last dimension is contiguous."""
+    rows, vocab = logits.shape
+    if vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("the logits of a row have to lie side by side")
+    return lib.card_logprobs(_ptr(logits), _type(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(tokens_dev),
+                             temperature, top, _ptr(logprob_dev), _ptr(entropy_dev), _ptr(top_tokens_dev), _ptr(top_logprobs_dev),
+                             _ptr(workspace_dev), _ptr(stream))
+
+
 def card_profile_enable(max_launches: int) -> int:
     return lib.card_profile_enable(max_launches)
 
@@ -364,6 +448,8 @@ def card_profile_collect(max_launches: int):
 
 
 def _i32(seq):
+    if isinstance(seq, C.Array) and seq._type_ is C.c_int32:
+        return seq
     return (C.c_int32 * len(seq))(*[int(v) for v in seq])
 
 

@@ -9,6 +9,7 @@ ROOT = os.path.dirname(PKG_DIR)
 LIB_PATH = os.path.join(PKG_DIR, "libcard.so")
 SOURCES = [
     os.path.join(PKG_DIR, "csrc", "card_api.hip"),
+    os.path.join(PKG_DIR, "csrc", "card_serving.hip"),
     os.path.join(PKG_DIR, "csrc", "card_cache.cpp"),
 ]
 

@@ -1,0 +1,211 @@
+// C ABI of what serves several sequences from one pair of page pools: argument checks and launches of page copies, slot
+// moves, attention over a ragged batch and log probabilities.
+#include <algorithm>
+#include <cmath>
+#include <cstdlib>
+#include <hip/hip_runtime.h>
+
+#include "card.h"
+#include "card_attend.hip"
+#include "card_logprobs.hip"
+#include "card_pages.hip"
+
+using namespace card;
+
+namespace {
+
+inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? CARD_OK : CARD_EDEVICE; }
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+inline size_t layer_elems(const card_model_cfg* cfg, int32_t n_pages) { return size_t(n_pages) * cfg->n_kv_heads * 16 * cfg->head_dim; }
+
+// A set of numbers >= 0, open addressing.
+class NumberSet {
+public:
+    explicit NumberSet(int32_t n) {
+        while (size_ < 2 * size_t(n)) size_ *= 2;
+        at_ = static_cast<int32_t*>(malloc(size_ * sizeof(int32_t)));
+        if (at_) std::fill(at_, at_ + size_, -1);
+    }
+    ~NumberSet() { free(at_); }
+    NumberSet(const NumberSet&) = delete;
+    NumberSet& operator=(const NumberSet&) = delete;
+    bool ok() const { return at_ != nullptr; }
+    bool has(int32_t v) const { return at_[place(v)] == v; }
+    bool add(int32_t v) {  // false: it was there
+        int32_t& p = at_[place(v)];
+        if (p == v) return false;
+        p = v;
+        return true;
+    }
+
+private:
+    size_t place(int32_t v) const {
+        size_t i = (uint32_t(v) * 0x9e3779b1u) & (size_ - 1);
+        while (at_[i] != -1 && at_[i] != v) i = (i + 1) & (size_ - 1);
+        return i;
+    }
+    size_t size_ = 16;
+    int32_t* at_ = nullptr;
+};
+
+int pool_args(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src, const int32_t* dst) {
+    if (!cfg_valid(cfg) || !kv || !kv->k_pages || !kv->v_pages || kv->n_pages <= 0 || n < 0) return CARD_EINVAL;
+    if (n > 0 && (!src || !dst)) return CARD_EINVAL;
+    if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages)) return CARD_EINVAL;
+    return CARD_OK;
+}
+
+bool rows_ok(const card_rows* r, int32_t type, int64_t least_stride) {
+    const int64_t unit = type == CARD_F32 ? 4 : 8;
+    return r && r->data && r->type == type && aligned16(r->data) && r->row_stride >= least_stride && r->head_stride >= least_stride &&
+           r->row_stride % unit == 0 && r->head_stride % unit == 0;
+}
+
+bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
+    return cfg_valid(cfg) && b && b->n_pages > 0 && b->n_seqs > 0 && b->table_pages > 0 && b->table_pages < (1 << 27) && b->n_rows >= 0 &&
+           b->max_new >= 0 && b->max_len >= 0;
+}
+
+template <int H, typename T>
+void attend_launch(const AttendArgs& a, hipStream_t st) {
+    if (a.k)
+        hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
+    hipLaunchKernelGGL((k_attend<H, T>), dim3(uint32_t(int64_t(a.n_rows) * a.G / 16 + a.n_seqs), uint32_t(a.Hkv)), dim3(64), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                       void* stream) {
+    if (const int st = pool_args(cfg, kv, n, src_host, dst_host)) return st;
+    if (n == 0) return CARD_OK;
+    NumberSet written(n);
+    if (!written.ok()) return CARD_EDEVICE;
+    for (int i = 0; i < n; ++i) {
+        if (src_host[i] < 0 || src_host[i] >= kv->n_pages || dst_host[i] < 0 || dst_host[i] >= kv->n_pages) return CARD_ERANGE;
+        if (!written.add(dst_host[i])) return CARD_EINVAL;
+    }
+    for (int i = 0; i < n; ++i)
+        if (written.has(src_host[i])) return CARD_EINVAL;
+    CopyArgs a = {};
+    a.pool[0] = static_cast<uint4v*>(kv->k_pages);
+    a.pool[1] = static_cast<uint4v*>(kv->v_pages);
+    a.layer16 = layer_elems(cfg, kv->n_pages) / 8;
+    a.page16 = cfg->n_kv_heads * 2 * cfg->head_dim;
+    for (int i = 0; i < n; i += kCopyPairs) {
+        const int m = std::min(n - i, kCopyPairs);
+        std::copy(src_host + i, src_host + i + m, a.src);
+        std::copy(dst_host + i, dst_host + i + m, a.dst);
+        hipLaunchKernelGGL(k_kv_copy_pages, dim3(uint32_t(m), uint32_t(cfg->n_layers), 2), dim3(256), 0, as_stream(stream), a);
+    }
+    return launch_status();
+}
+
+int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                       void* stream) {
+    if (const int st = pool_args(cfg, kv, n, src_host, dst_host)) return st;
+    if (n == 0) return CARD_OK;
+    NumberSet written(n);
+    if (!written.ok()) return CARD_EDEVICE;
+    const int64_t slots = int64_t(kv->n_pages) * 16;
+    for (int i = 0; i < n; ++i) {
+        if (src_host[i] < 0 || src_host[i] >= slots || dst_host[i] < 0 || dst_host[i] >= slots) return CARD_ERANGE;
+        if (written.has(src_host[i]) || !written.add(dst_host[i])) return CARD_EINVAL;
+    }
+    MoveArgs a = {};
+    a.kpool = static_cast<__bf16*>(kv->k_pages);
+    a.vpool = static_cast<__bf16*>(kv->v_pages);
+    a.layer_elems = layer_elems(cfg, kv->n_pages);
+    a.n_kv_heads = cfg->n_kv_heads;
+    a.head_dim = cfg->head_dim;
+    for (int i = 0; i < n; i += kMoveSlots) {
+        a.n = std::min(n - i, kMoveSlots);
+        std::copy(src_host + i, src_host + i + a.n, a.src);
+        std::copy(dst_host + i, dst_host + i + a.n, a.dst);
+        hipLaunchKernelGGL(k_kv_move_slots, dim3(uint32_t(cfg->n_kv_heads), uint32_t(cfg->n_layers)), dim3(128), 0, as_stream(stream), a);
+    }
+    return launch_status();
+}
+
+size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch) {
+    return batch_ok(cfg, batch) ? 0 : 0;
+}
+
+int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
+                   const card_rows* v, const card_rows* out, const card_row_mask* mask, void* workspace_dev, void* stream) {
+    if (!batch_ok(cfg, batch)) return CARD_EINVAL;
+    if (!batch->k_pages || !batch->v_pages || !batch->block_tables || !batch->ctx_lens || !batch->row_starts) return CARD_EINVAL;
+    if (!aligned16(batch->k_pages) || !aligned16(batch->v_pages)) return CARD_EINVAL;
+    if (layer < 0 || layer >= cfg->n_layers) return CARD_ERANGE;
+    if (int64_t(batch->n_rows) * cfg->n_q_heads + batch->n_seqs >= (int64_t(1) << 31)) return CARD_ERANGE;
+    if (batch->n_rows == 0) return CARD_OK;
+    if (!q || !out || (q->type != CARD_BF16 && q->type != CARD_F32)) return CARD_EINVAL;
+    if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
+    if (k && (!rows_ok(k, q->type, 0) || !rows_ok(v, q->type, 0))) return CARD_EINVAL;
+    if (mask && (!mask->mask_dev || !mask->mask_base_dev || mask->words < 1 || mask->words > (1 << 25))) return CARD_EINVAL;
+    (void)workspace_dev;
+    AttendArgs a = {};
+    a.q = q->data;
+    a.q_row = q->row_stride;
+    a.q_head = q->head_stride;
+    if (k) {
+        a.k = k->data;
+        a.k_row = k->row_stride;
+        a.k_head = k->head_stride;
+        a.v = v->data;
+        a.v_row = v->row_stride;
+        a.v_head = v->head_stride;
+    }
+    a.out = out->data;
+    a.o_row = out->row_stride;
+    a.o_head = out->head_stride;
+    a.kpool = static_cast<__bf16*>(batch->k_pages) + size_t(layer) * layer_elems(cfg, batch->n_pages);
+    a.vpool = static_cast<__bf16*>(batch->v_pages) + size_t(layer) * layer_elems(cfg, batch->n_pages);
+    a.tables = batch->block_tables;
+    a.ctx = batch->ctx_lens;
+    a.starts = batch->row_starts;
+    a.table_pages = batch->table_pages;
+    a.n_pages = batch->n_pages;
+    a.n_seqs = batch->n_seqs;
+    a.n_rows = batch->n_rows;
+    a.Hkv = cfg->n_kv_heads;
+    a.G = cfg->n_q_heads / cfg->n_kv_heads;
+    if (mask) {
+        a.mask = mask->mask_dev;
+        a.mask_base = mask->mask_base_dev;
+        a.mask_words = mask->words;
+    }
+    a.scale = 1.4426950408889634f / sqrtf(float(cfg->head_dim));
+    hipStream_t st = as_stream(stream);
+    const bool wide = cfg->head_dim == 128;
+    if (q->type == CARD_F32) wide ? attend_launch<128, float>(a, st) : attend_launch<64, float>(a, st);
+    else wide ? attend_launch<128, __bf16>(a, st) : attend_launch<64, __bf16>(a, st);
+    return launch_status();
+}
+
+size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
+    (void)rows, (void)vocab, (void)top;
+    return 0;
+}
+
+int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens_dev,
+                  float temperature, int32_t top, float* logprob_dev, float* entropy_dev, int32_t* top_tokens_dev,
+                  float* top_logprobs_dev, void* workspace_dev, void* stream) {
+    if ((type != CARD_BF16 && type != CARD_F32) || rows < 0 || vocab < 1 || row_stride < vocab) return CARD_EINVAL;
+    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature)) return CARD_EINVAL;
+    if (top < 0 || top > kMaxTop) return CARD_ERANGE;
+    if (rows == 0) return CARD_OK;
+    if (!logits_dev || !tokens_dev != !logprob_dev || (top > 0 && (!top_tokens_dev || !top_logprobs_dev))) return CARD_EINVAL;
+    if (!tokens_dev && !entropy_dev && top == 0) return CARD_EINVAL;
+    (void)workspace_dev;
+    const LogprobArgs a = {logits_dev,  row_stride,  vocab,          top,             tokens_dev, 1.0f / temperature,
+                           logprob_dev, entropy_dev, top_tokens_dev, top_logprobs_dev};
+    if (type == CARD_F32) hipLaunchKernelGGL(k_logprobs<float>, dim3(uint32_t(rows)), dim3(256), 0, as_stream(stream), a);
+    else hipLaunchKernelGGL(k_logprobs<__bf16>, dim3(uint32_t(rows)), dim3(256), 0, as_stream(stream), a);
+    return launch_status();
+}
+
+}  // extern "C"
