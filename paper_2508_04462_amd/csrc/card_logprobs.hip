@@ -1,10 +1,16 @@
 // Log probabilities, entropies and most probable tokens of rows of logits.
+//
+// One pass over a row: with m the largest logit so far and d = (x - m) / T, s = sum e^d and t = sum d e^d are rescaled as m grows;
+// ln p = d - ln s and the entropy is ln s - t / s.  d is taken from the difference, not from x / T - m / T: far from
+// zero those two lose what the difference keeps.  Bound by reading the logits.
 #pragma once
 #include "card_common.hip"
 
 namespace card {
 
 constexpr int kMaxTop = 32;
+constexpr int kLpThreads = 256, kLpWaves = 4;
+constexpr int kLpVecs = 4;  // 16-byte loads of a lane in flight
 
 struct LogprobArgs {
     const void* logits;
@@ -16,73 +22,223 @@ struct LogprobArgs {
     float* entropy;
     int32_t* top_tokens;
     float* top_logprobs;
+    // a row in several parts: 16-byte units of a part, parts, and what each of them leaves: sums [row][part][4], keys [row][part][top]
+    int32_t part_vecs, parts;
+    float* part_sums;
+    unsigned long long* part_keys;
 };
 
 __device__ __forceinline__ float logit_at(const float* p, int i) { return p[i]; }
 __device__ __forceinline__ float logit_at(const __bf16* p, int i) { return static_cast<float>(p[i]); }
-
-// (max, sum of e^d, sum of d e^d) of one part of a row, d = (x - max) / T; a NaN anywhere is in the sum.
-struct RowSums {
-    float m, s, t;
-};
-// d is kept finite where it meets e^d = 0: a logit of -inf (or far below) has no part in either sum
-__device__ __forceinline__ RowSums join_sums(RowSums a, RowSums b, float inv_temp) {
-    const float m = fmaxf(a.m, b.m);
-    const float da = fmaxf((a.m - m) * inv_temp, -1e4f), db = fmaxf((b.m - m) * inv_temp, -1e4f);
-    const float ea = expf((a.m - m) * inv_temp), eb = expf((b.m - m) * inv_temp);
-    return {m, a.s * ea + b.s * eb, (a.t + a.s * da) * ea + (b.t + b.s * db) * eb};
+__device__ __forceinline__ void unpack_logits(uint4v w, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ void unpack_logits(uint4v w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
 }
 
-// One workgroup: one row; a pass for the sums, then one for each of the most probable tokens.
-template <typename T>
-__global__ __launch_bounds__(256) void k_logprobs(LogprobArgs a) {
-    __shared__ RowSums sums[256];
-    __shared__ unsigned long long best[256];
-    const int row = blockIdx.x, tid = threadIdx.x;
-    const T* x = static_cast<const T*>(a.logits) + int64_t(row) * a.row_stride;
-    RowSums r = {-3.402823466e38f, 0.f, 0.f};
-    for (int i = tid; i < a.vocab; i += 256) r = join_sums(r, RowSums{logit_at(x, i) == -INFINITY ? -3.402823466e38f : logit_at(x, i), logit_at(x, i) == -INFINITY ? 0.f : 1.f, 0.f}, a.inv_temp);
-    sums[tid] = r;
-    __syncthreads();
-    for (int d = 128; d > 0; d >>= 1) {
-        if (tid < d) sums[tid] = join_sums(sums[tid], sums[tid + d], a.inv_temp);
-        __syncthreads();
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.402823466e38f;  // m before any logit; a logit of -inf then has d = -inf and no part in s or t
+
+// Of some logits: largest, sum of 2^d and sum of d 2^d, d = (x - m) log2(e) / T.  A NaN or +inf among them makes s NaN.
+// d is kept finite where it meets 2^d = 0.
+struct RowSums {
+    float m, s, t;
+    __device__ __forceinline__ void raise(float mnew, float c) {
+        const float d = (m - mnew) * c, e = __builtin_amdgcn_exp2f(d);
+        t = (t + s * fmaxf(d, -1e4f)) * e;
+        s *= e;
+        m = mnew;
     }
-    r = sums[0];
+    __device__ __forceinline__ void add(float x, float c) {
+        const float d = (x - m) * c, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        t = fmaf(e, fmaxf(d, -1e4f), t);
+    }
+    __device__ __forceinline__ void join(RowSums b, float c) {
+        const float mnew = fmaxf(m, b.m);
+        raise(mnew, c);
+        b.raise(mnew, c);
+        s += b.s;
+        t += b.t;
+    }
+};
+__device__ __forceinline__ RowSums join_lanes(RowSums r, float c) {
+    for (int d = 1; d < 64; d <<= 1) r.join(RowSums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.t, d)}, c);
+    return r;
+}
+
+// The largest keys that a wavefront has been offered, in order: lane i holds the i-th of them, `least` is number top - 1.  Keys are
+// a logit in the upper half, the complement of its token in the lower one: unique, and equal logits order by token.
+// An offer costs a comparison and a ballot; a key that enters, about 100 clocks.  Of n keys in random order top * ln(n / top) enter.
+__device__ __forceinline__ unsigned long long lane_key(unsigned long long v, int lane) {
+    return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v)), lane))) |
+           (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v >> 32)), lane))) << 32);
+}
+struct TopList {
+    unsigned long long best = 0ull, least = 0ull;
+    __device__ __forceinline__ void offer(unsigned long long key, int top, int lane) {
+        unsigned long long in = __ballot(key > least);
+        while (in) {
+            const unsigned long long k = lane_key(key, __ffsll(in) - 1);
+            const int at = __popcll(__ballot(best > k));
+            const unsigned long long up = __shfl_up(best, 1);
+            best = lane < at ? best : (lane == at ? k : up);
+            least = lane_key(best, top - 1);
+            in &= in - 1;
+            in &= __ballot(key > least);
+        }
+    }
+};
+__device__ __forceinline__ unsigned long long logit_key(float x, int token) {
+    // (-0 and 0 are equal; without probability: no key)
+    return x == -INFINITY ? 0ull : (uint64_t(float_key(x + 0.f)) << 32) | (0xffffffffu - uint32_t(token));
+}
+
+struct LogprobShared {
+    float sums[kLpWaves][3];
+    unsigned long long keys[kLpWaves * kMaxTop], out[kMaxTop];
+};
+
+// The wavefronts' sums and lists become the workgroup's: returned, and in sm.out.
+__device__ __forceinline__ RowSums join_waves(LogprobShared& sm, RowSums r, const TopList& list, int top, float c) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    r = join_lanes(r, c);
+    if (lane == 0) {
+        sm.sums[wave][0] = r.m;
+        sm.sums[wave][1] = r.s;
+        sm.sums[wave][2] = r.t;
+    }
+    if (lane < top) sm.keys[wave * top + lane] = list.best;
+    if (tid < top) sm.out[tid] = 0ull;
+    __syncthreads();
+    r = {sm.sums[0][0], sm.sums[0][1], sm.sums[0][2]};
+#pragma unroll
+    for (int w = 1; w < kLpWaves; ++w) r.join(RowSums{sm.sums[w][0], sm.sums[w][1], sm.sums[w][2]}, c);
+    if (tid < kLpWaves * top && sm.keys[tid] != 0ull) {  // the place of a key: how many are larger
+        const unsigned long long k = sm.keys[tid];
+        int larger = 0;
+        for (int i = 0; i < kLpWaves * top; ++i) larger += sm.keys[i] > k;
+        if (larger < top) sm.out[larger] = k;
+    }
+    __syncthreads();
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, const LogprobShared& sm, RowSums r, int row) {
+    const int tid = threadIdx.x;
+    const T* x = static_cast<const T*>(a.logits) + int64_t(row) * a.row_stride;
     const float ln_s = logf(r.s);
-    const bool is_void = r.s != r.s || r.m == INFINITY, empty = r.s == 0.f;
+    const bool is_void = r.s != r.s, empty = r.s == 0.f;
     const auto logprob = [&](float v) { return is_void ? NAN : (empty ? -INFINITY : (v - r.m) * a.inv_temp - ln_s); };
-    if (tid == 0) {
+    if (tid < a.top) {
+        const unsigned long long key = sm.out[tid];
+        const bool none = is_void || key == 0ull;
+        const uint32_t f = uint32_t(key >> 32);
+        const float v = __uint_as_float(f & 0x80000000u ? f ^ 0x80000000u : ~f);
+        a.top_tokens[int64_t(row) * a.top + tid] = none ? -1 : int(0xffffffffu - uint32_t(key));
+        a.top_logprobs[int64_t(row) * a.top + tid] = none ? (is_void ? NAN : -INFINITY) : logprob(v);
+    }
+    if (tid == 64) {  // (another wavefront than the one above)
         if (a.tokens) {
             const int tok = a.tokens[row];
             a.logprob[row] = tok < 0 ? 0.f : (tok >= a.vocab ? NAN : logprob(logit_at(x, tok)));
         }
-        if (a.entropy) a.entropy[row] = is_void ? NAN : (empty ? 0.f : ln_s - r.t / r.s);
+        if (a.entropy) a.entropy[row] = is_void ? NAN : (empty ? 0.f : ln_s - r.t / r.s * kLn2);
     }
-    unsigned long long below = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-        unsigned long long b = 0ull;
-        for (int i = tid; i < a.vocab; i += 256) {
-            const float v = logit_at(x, i);
-            const unsigned long long key = (static_cast<unsigned long long>(float_key(v + 0.f)) << 32) | (0xffffffffu - uint32_t(i));
-            if (v > -INFINITY && key < below && key > b) b = key;
+}
+
+// One workgroup: one part of one row, in turns of kLpVecs 16-byte loads a lane.  The loads are of aligned units, whatever the row begins at:
+// what a unit holds before the row or behind it is not read.
+template <typename T>
+__global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
+    constexpr int VN = 16 / sizeof(T);
+    __shared__ LogprobShared sm;
+    const int row = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float c = a.inv_temp * kLog2e;
+    const T* x0 = static_cast<const T*>(a.logits) + int64_t(row) * a.row_stride;
+    const int lead = int(reinterpret_cast<uintptr_t>(x0) % 16 / sizeof(T));  // logits of the first unit that are not the row's
+    const uint4v* units = reinterpret_cast<const uint4v*>(x0 - lead);
+    const int n_units = (lead + a.vocab + VN - 1) / VN, end = min(n_units, (part + 1) * a.part_vecs);
+    RowSums r = {kLowest, 0.f, 0.f};
+    TopList list;
+    for (int first = part * a.part_vecs + wave * 64 * kLpVecs; first < end; first += kLpThreads * kLpVecs) {
+        float x[kLpVecs][VN];
+        if (first * VN >= lead && (first + 64 * kLpVecs) * VN <= lead + a.vocab && first + 64 * kLpVecs <= end) {
+            uint4v w[kLpVecs];
+#pragma unroll
+            for (int u = 0; u < kLpVecs; ++u) w[u] = units[first + u * 64 + lane];
+#pragma unroll
+            for (int u = 0; u < kLpVecs; ++u) unpack_logits(w[u], x[u]);
+        } else {  // the ends of the row or of the part
+#pragma unroll
+            for (int u = 0; u < kLpVecs; ++u) {
+                const int unit = first + u * 64 + lane;
+#pragma unroll
+                for (int e = 0; e < VN; ++e) {
+                    const int i = unit * VN + e - lead;
+                    x[u][e] = unit < end && i >= 0 && i < a.vocab ? logit_at(x0, i) : -INFINITY;
+                }
+            }
         }
-        best[tid] = b;
-        __syncthreads();
-        for (int d = 128; d > 0; d >>= 1) {
-            if (tid < d && best[tid + d] > best[tid]) best[tid] = best[tid + d];
-            __syncthreads();
+        float most[kLpVecs];
+#pragma unroll
+        for (int u = 0; u < kLpVecs; ++u) {
+            most[u] = x[u][0];
+#pragma unroll
+            for (int e = 1; e < VN; ++e) most[u] = fmaxf(most[u], x[u][e]);
         }
-        b = best[0];
-        __syncthreads();
-        if (tid == 0) {
-            const int tok = int(0xffffffffu - uint32_t(b));
-            const bool none = b == 0ull || is_void;
-            a.top_tokens[int64_t(row) * a.top + k] = none ? -1 : tok;
-            a.top_logprobs[int64_t(row) * a.top + k] = is_void ? NAN : (none ? -INFINITY : logprob(logit_at(x, tok)));
+        float all = most[0];
+#pragma unroll
+        for (int u = 1; u < kLpVecs; ++u) all = fmaxf(all, most[u]);
+        r.raise(fmaxf(r.m, all), c);
+#pragma unroll
+        for (int u = 0; u < kLpVecs; ++u)
+#pragma unroll
+            for (int e = 0; e < VN; ++e) r.add(x[u][e], c);
+        // (tokens of later turns are larger: an equal logit does not enter; inside a turn it may)
+        if (a.top > 0 && __ballot(float_key(all + 0.f) > uint32_t(list.least >> 32))) {
+#pragma unroll
+            for (int u = 0; u < kLpVecs; ++u) {
+                if (!__ballot(float_key(most[u] + 0.f) >= uint32_t(list.least >> 32))) continue;
+#pragma unroll
+                for (int e = 0; e < VN; ++e) list.offer(logit_key(x[u][e], (first + u * 64 + lane) * VN + e - lead), a.top, lane);
+            }
         }
-        below = b;
     }
+    r = join_waves(sm, r, list, a.top, c);
+    if (a.parts == 1) {
+        finish_row<T>(a, sm, r, row);
+        return;
+    }
+    const size_t at = size_t(row) * a.parts + part;
+    if (tid == 0) *reinterpret_cast<floatx4*>(a.part_sums + at * 4) = floatx4{r.m, r.s, r.t, 0.f};
+    if (tid < a.top) a.part_keys[at * a.top + tid] = sm.out[tid];
+}
+
+// One workgroup: the parts of a row.
+template <typename T>
+__global__ __launch_bounds__(kLpThreads) void k_logprobs_join(LogprobArgs a) {
+    __shared__ LogprobShared sm;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, n = a.parts * a.top;
+    const float c = a.inv_temp * kLog2e;
+    RowSums r = {kLowest, 0.f, 0.f};
+    for (int p = tid; p < a.parts; p += kLpThreads) {
+        const floatx4 v = *reinterpret_cast<const floatx4*>(a.part_sums + (size_t(row) * a.parts + p) * 4);
+        r.join(RowSums{v[0], v[1], v[2]}, c);
+    }
+    TopList list;
+    for (int i = tid - lane; i < n; i += kLpThreads)
+        list.offer(i + lane < n ? a.part_keys[size_t(row) * n + i + lane] : 0ull, a.top, lane);
+    r = join_waves(sm, r, list, a.top, c);
+    finish_row<T>(a, sm, r, row);
 }
 
 }  // namespace card

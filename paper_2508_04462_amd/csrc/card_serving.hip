@@ -67,6 +67,17 @@ bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
            b->max_new >= 0 && b->max_len >= 0;
 }
 
+// How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more.
+int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(1024, rows)); }
+size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
+
+template <typename T>
+int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
+    hipLaunchKernelGGL(k_logprobs<T>, dim3(uint32_t(rows), uint32_t(a.parts)), dim3(kLpThreads), 0, st, a);
+    if (a.parts > 1) hipLaunchKernelGGL(k_logprobs_join<T>, dim3(uint32_t(rows)), dim3(kLpThreads), 0, st, a);
+    return launch_status();
+}
+
 template <int H, typename T>
 void attend_launch(const AttendArgs& a, hipStream_t st) {
     if (a.k)
@@ -187,25 +198,31 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
 }
 
 size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
-    (void)rows, (void)vocab, (void)top;
-    return 0;
+    if (rows < 1 || vocab < 1 || top < 0 || top > kMaxTop || logprob_parts(rows, vocab) == 1) return 0;
+    return logprob_sums_bytes(rows, vocab) + size_t(rows) * logprob_parts(rows, vocab) * top * 8;
 }
 
 int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens_dev,
                   float temperature, int32_t top, float* logprob_dev, float* entropy_dev, int32_t* top_tokens_dev,
                   float* top_logprobs_dev, void* workspace_dev, void* stream) {
     if ((type != CARD_BF16 && type != CARD_F32) || rows < 0 || vocab < 1 || row_stride < vocab) return CARD_EINVAL;
-    if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.0f / temperature)) return CARD_EINVAL;
+    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return CARD_EINVAL;
     if (top < 0 || top > kMaxTop) return CARD_ERANGE;
     if (rows == 0) return CARD_OK;
     if (!logits_dev || !tokens_dev != !logprob_dev || (top > 0 && (!top_tokens_dev || !top_logprobs_dev))) return CARD_EINVAL;
     if (!tokens_dev && !entropy_dev && top == 0) return CARD_EINVAL;
-    (void)workspace_dev;
-    const LogprobArgs a = {logits_dev,  row_stride,  vocab,          top,             tokens_dev, 1.0f / temperature,
-                           logprob_dev, entropy_dev, top_tokens_dev, top_logprobs_dev};
-    if (type == CARD_F32) hipLaunchKernelGGL(k_logprobs<float>, dim3(uint32_t(rows)), dim3(256), 0, as_stream(stream), a);
-    else hipLaunchKernelGGL(k_logprobs<__bf16>, dim3(uint32_t(rows)), dim3(256), 0, as_stream(stream), a);
-    return launch_status();
+    const int parts = logprob_parts(rows, vocab);
+    if (parts > 1 && (!workspace_dev || !aligned16(workspace_dev))) return CARD_EINVAL;
+    LogprobArgs a = {logits_dev,  row_stride,  vocab,          top,             tokens_dev, 1.0f / temperature,
+                     logprob_dev, entropy_dev, top_tokens_dev, top_logprobs_dev};
+    const int units = vocab / (type == CARD_F32 ? 4 : 8) + 2;  // of 16 bytes, the ends of a row that begins anywhere among them
+    a.part_vecs = ceil_div(units, parts);
+    a.parts = ceil_div(units, a.part_vecs);
+    if (parts > 1) {
+        a.part_sums = static_cast<float*>(workspace_dev);
+        a.part_keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace_dev) + logprob_sums_bytes(rows, vocab));
+    }
+    return type == CARD_F32 ? logprobs_launch<float>(a, rows, as_stream(stream)) : logprobs_launch<__bf16>(a, rows, as_stream(stream));
 }
 
 }  // extern "C"
