@@ -1,5 +1,7 @@
 // Attention of the new tokens of a ragged batch over one paged cache.
 #pragma once
+#include <type_traits>
+
 #include "card_common.hip"
 
 namespace card {
@@ -22,11 +24,9 @@ struct AttendArgs {
     const int32_t* mask_base;
     int32_t mask_words;
     float scale;  // log2(e) / sqrt(head size): the softmax runs on exp2
-    // the pages of a sequence in up to `cuts` cuts of cut_pages or more; where there are several: their partial results and how many have
-    // arrived, per unit and KV head (counters; cleared by the kernel that stores the keys)
-    int32_t cuts, cut_pages, counters;
+    // the pages of a sequence in up to `cuts` cuts of cut_pages or more, and their partial results where there are several
+    int32_t cuts, cut_pages;
     float* part;
-    uint32_t* arrived;
 };
 
 // The sequence and the part of it that unit number `unit` of a launch is about.  Units are dealt so that no prefix sum is needed:
@@ -59,13 +59,11 @@ __device__ __forceinline__ SeqUnit find_unit(const AttendArgs& a, int unit, int 
     return u;
 }
 
-// Clears the arrival counters; keys and values of the new tokens go to their pages.  One workgroup: one page of one KV head.  A thread writes the 8 elements of a token
+// Keys and values of the new tokens go to their pages.  One workgroup: one page of one KV head.  A thread writes the 8 elements of a token
 // that lie together in K, or the 4 tokens of an element that lie together in V.
 constexpr int kStoreUnits = 2;  // pages per sequence beyond its new tokens / 16
 template <typename T>
 __global__ __launch_bounds__(256) void k_attend_store(AttendArgs a, int h) {
-    for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < a.counters; i += gridDim.x * gridDim.y * 256) a.arrived[i] = 0u;
-    if (!a.k) return;
     const SeqUnit u = find_unit(a, blockIdx.x, 1, 16, kStoreUnits);
     if (u.index < 0 || u.len <= u.ctx) return;
     const int pg = (u.ctx >> 4) + u.index, slot0 = pg * 16, head = blockIdx.y;
@@ -153,45 +151,95 @@ __device__ __forceinline__ void load_k_page(const AttendArgs& a, int id, int kvh
     for (int st = 0; st < H / 32; ++st) k[st] = p[st * 64];
 }
 template <int H>
-__device__ __forceinline__ void load_v_page(const AttendArgs& a, int id, int kvh, int lane, short4v (&v)[H / 16]) {
+__device__ __forceinline__ void load_v_page(const AttendArgs& a, int id, int kvh, int lane, uint2v (&v)[H / 16]) {
     const uint4v* p = reinterpret_cast<const uint4v*>(a.vpool + (size_t(id) * a.Hkv + kvh) * (16 * H)) + lane;
 #pragma unroll
     for (int i = 0; i < H / 32; ++i) {
         const uint4v w = p[i * 64];
-        v[2 * i] = __builtin_bit_cast(short4v, uint2v{w[0], w[1]});
-        v[2 * i + 1] = __builtin_bit_cast(short4v, uint2v{w[2], w[3]});
+        v[2 * i] = uint2v{w[0], w[1]};
+        v[2 * i + 1] = uint2v{w[2], w[3]};
+    }
+}
+// Of four values of 16 bits: those below number n, as a mask.
+__device__ __forceinline__ uint2v first_of_four(int n) {
+    return uint2v{(n > 0 ? 0xffffu : 0u) | (n > 1 ? 0xffff0000u : 0u), (n > 2 ? 0xffffu : 0u) | (n > 3 ? 0xffff0000u : 0u)};
+}
+__device__ __forceinline__ uint32_t bf16_bits(__bf16 v) { return __builtin_bit_cast(unsigned short, v); }
+
+// A page that new tokens belong to: their keys and values come from the call's arrays, whoever of the workgroups that read the page stores
+// them in it.  Tokens [own0, own1) are this wavefront's to store.
+template <int H, typename T>
+__device__ __forceinline__ void take_new_tokens(const AttendArgs& a, const SeqUnit& u, int id, int kvh, int slot, int lane, int own0, int own1,
+                                                bf16x8 (&k)[H / 32], uint2v (&v)[H / 16]) {
+    const int col = lane & 15, t0 = slot + (lane >> 4) * 4;
+    const size_t page = (size_t(id) * a.Hkv + kvh) * (16 * H);
+    const int tok = slot + col;
+    const bool fresh = tok >= u.ctx && tok < u.len;
+    const T* p = static_cast<const T*>(a.k) + int64_t(u.row0 + (fresh ? tok - u.ctx : 0)) * a.k_row + int64_t(kvh) * a.k_head + (lane >> 4) * 8;
+#pragma unroll
+    for (int st = 0; st < H / 32; ++st) {
+        bf16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = static_cast<__bf16>(p[st * 32 + e]);
+        k[st] = fresh ? w : k[st];
+        if (fresh && tok >= own0 && tok < own1) *(reinterpret_cast<bf16x8*>(a.kpool + page) + st * 64 + lane) = w;
+    }
+    const T* pv[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        pv[e] = static_cast<const T*>(a.v) + int64_t(u.row0 + min(max(t0 + e - u.ctx, 0), u.n_new - 1)) * a.v_row + int64_t(kvh) * a.v_head + col;
+    const uint2v below = first_of_four(u.len - t0), old = first_of_four(u.ctx - t0), take = {below[0] & ~old[0], below[1] & ~old[1]};
+#pragma unroll
+    for (int i = 0; i < H / 16; ++i) {
+        __bf16 w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = static_cast<__bf16>(pv[e][i * 16]);
+        v[i][0] = (v[i][0] & ~take[0]) | ((bf16_bits(w[0]) | bf16_bits(w[1]) << 16) & take[0]);
+        v[i][1] = (v[i][1] & ~take[1]) | ((bf16_bits(w[2]) | bf16_bits(w[3]) << 16) & take[1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (t0 + e >= own0 && t0 + e < min(own1, u.len)) a.vpool[page + (i >> 1) * 512 + lane * 8 + (i & 1) * 4 + e] = w[e];
     }
 }
 
-constexpr int kAuxDev = 16;  // device scope
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t dev_rsrc(const void* base) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, 0xffffffffu, 0x00020000);
+// The pages that rows up to token m_last see, and their cuts.
+struct UnitCuts {
+    int32_t all_pages, pages, n;
+};
+__device__ __forceinline__ UnitCuts cuts_of(const AttendArgs& a, const SeqUnit& u, int m_last) {
+    UnitCuts c;
+    c.all_pages = ((a.mask ? u.len : min(u.ctx + m_last + 1, u.len)) + 15) >> 4;
+    c.pages = max(a.cut_pages, (c.all_pages + a.cuts - 1) / a.cuts);
+    c.n = (c.all_pages + c.pages - 1) / c.pages;
+    return c;
 }
+
+// Floats that a cut leaves of a tile: [16][H], [16] maxima, [16] sums.
+template <int H>
+constexpr int kPartFloats = 16 * (H + 2);
 
 // For few rows per sequence (16 NT rows x heads of a KV head at a time): bound by reading the cache, so every page is read once, straight into
 // the registers that the matrix instructions take it from.  One workgroup: one cut of the pages of a sequence, for one KV head; its four
 // wavefronts take every fourth page each, two per round, and refill K as soon as the scores are done, V behind P V.  The wavefronts' results
-// meet in LDS, the cuts' in memory: the last one to arrive adds them up, in their order.
-template <int H, typename T, int NT>
+// meet in LDS, the cuts' in memory, where k_attend_join adds them up.
+// NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 5 us.
+template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4 ? 2 : 1)) void k_attend_few(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, LD = H + 4, CH = H / 16;
     __shared__ __align__(16) float red[4][16][LD];
     __shared__ float red_m[4][16], red_l[4][16];
-    __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, kvh = blockIdx.y, cut = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const SeqUnit u = find_unit(a, blockIdx.x, a.G, 16 * NT, 1);
     const int R = u.n_new * a.G, rho0 = u.index * 16 * NT;
     if (u.index < 0 || rho0 >= R) return;
-    // the pages that the last of the rows sees, and this cut's part of them
     const int m_first = rho0 / a.G, m_last = (min(rho0 + 16 * NT, R) - 1) / a.G;
-    const int n_keys = a.mask ? u.len : min(u.ctx + m_last + 1, u.len);
-    const int n_pages = (n_keys + 15) >> 4;
-    const int per_cut = max(a.cut_pages, (n_pages + a.cuts - 1) / a.cuts), n_cuts = (n_pages + per_cut - 1) / per_cut;
-    if (cut >= n_cuts) return;
-    const int p0 = cut * per_cut + wave, p1 = min(n_pages, cut * per_cut + per_cut);
+    const UnitCuts uc = cuts_of(a, u, m_last);
+    if (cut >= uc.n) return;
+    const int p0 = cut * uc.pages + wave, p1 = min(uc.all_pages, (cut + 1) * uc.pages);
     const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
     const int all_see = a.mask ? min(base, u.len) : min(u.ctx + m_first + 1, u.len);  // slots below are seen by every row
+    const int own0 = u.ctx + (rho0 + a.G - 1) / a.G, own1 = u.ctx + m_last + 1;  // the tokens whose first head is among the rows
     Column c[NT];
     bf16x8 qf[NT][NP][ST];
     floatx4 o[NT][HT];
@@ -211,30 +259,38 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     const int count = p0 < p1 ? (p1 - p0 + 3) >> 2 : 0;
     const auto fetch_ids = [&](int i) { ids = i + lane < count ? table[p0 + 4 * (i + lane)] : -1; };
     const auto held = [&](int id) { return id >= 0 && id < a.n_pages; };
+    // pages that hold no new token and that every row sees whole come first, in pairs: their rounds have no memory access but the
+    // refills, which then stay in flight
+    const int plain_pages = min(NEW ? min(u.ctx, all_see) : all_see, u.len) >> 4;
+    const int plain = (p0 < min(p1, plain_pages) ? (min(p1, plain_pages) - p0 + 3) >> 2 : 0) & ~1;
     bf16x8 k[2][ST];
-    short4v v[2][HT];
+    uint2v v[2][HT];
     int id[2];
-    if (count > 0) {
-        fetch_ids(0);
+    const auto refill_k = [&](int i) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            id[j] = page_id(j);
+            id[j] = page_id(i + j);
             load_k_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, k[j]);
         }
+    };
+    const auto refill_v = [&]() {
 #pragma unroll
         for (int j = 0; j < 2; ++j) load_v_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, v[j]);
-    }
-    for (int i = 0; i < count; i += 2) {
+    };
+    const auto round = [&](int i, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
         int slot[2];
-        bool there[2], full = true;
+        bool there[2];  // (behind the last page id is -1)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             slot[j] = (p0 + 4 * (i + j)) * 16;
-            there[j] = held(id[j]);  // (behind the last page id is -1)
-            full = full && there[j] && slot[j] + 16 <= all_see;
+            there[j] = held(id[j]);
         }
-        short4v p[2][NT][NP];
-        float alpha[NT];
+        if constexpr (!WHOLE && NEW) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (there[j] && slot[j] + 16 > u.ctx) take_new_tokens<H, T>(a, u, id[j], kvh, slot[j], lane, own0, own1, k[j], v[j]);
+        }
         floatx4 s[2][NT];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -250,19 +306,23 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                     for (int n = 0; n < NT; ++n) s[j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][st], qf[n][w][st], s[j][n], 0, 0, 0);
         if (i + 2 < count) {
             if (((i + 2) & 63) == 0) fetch_ids(i + 2);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                id[j] = page_id(i + 2 + j);
-                load_k_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, k[j]);
-            }
+            refill_k(i + 2);
         }
+        const bool both = there[0] && there[1];
+        uint2v p[2][NT][NP];
+        float alpha[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            if (!full) {
+            if (!WHOLE || !both) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     bool ok[4];
-                    seen_keys(a, c[n].row, base, there[j] ? c[n].limit : -1, slot[j] + kq * 4, ok);
+                    if constexpr (WHOLE) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ok[e] = there[j];
+                    } else {
+                        seen_keys(a, c[n].row, base, there[j] ? c[n].limit : -1, slot[j] + kq * 4, ok);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[j][n][e] = ok[e] ? s[j][n][e] : -INFINITY;
                 }
@@ -282,24 +342,23 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = __builtin_amdgcn_exp2f(s[j][n][e] - mref);
-                    psum += x;
-                    __bf16 w[NP];
-                    split_parts<NP>(x, w);
+                for (int e = 0; e < 4; e += 2) {
+                    const float x0 = __builtin_amdgcn_exp2f(s[j][n][e] - mref), x1 = __builtin_amdgcn_exp2f(s[j][n][e + 1] - mref);
+                    psum += x0 + x1;
+                    __bf16 w0[NP], w1[NP];
+                    split_parts<NP>(x0, w0);
+                    split_parts<NP>(x1, w1);
 #pragma unroll
-                    for (int q = 0; q < NP; ++q) p[j][n][q][e] = __builtin_bit_cast(short, w[q]);
+                    for (int q = 0; q < NP; ++q) p[j][n][q][e / 2] = bf16_bits(w0[q]) | bf16_bits(w1[q]) << 16;
                 }
             sum[n] = sum[n] * alpha[n] + psum;  // (of this lane's keys; the four lanes of a column are added up at the end)
         }
-        if (!full) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
+        if (!WHOLE || !both) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int own = there[j] ? u.len - slot[j] - kq * 4 : 0;
+                const uint2v own = first_of_four(there[j] ? u.len - slot[j] - kq * 4 : 0);
 #pragma unroll
-                for (int t = 0; t < HT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[j][t][e] = e < own ? v[j][t][e] : short(0);
+                for (int t = 0; t < HT; ++t) v[j][t] &= own;
             }
         }
 #pragma unroll
@@ -313,16 +372,21 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
 #pragma unroll
                 for (int t = 0; t < HT; ++t)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v[j][t], p[j][n][q], o[n][t], 0, 0, 0);
-        if (i + 2 < count) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) load_v_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, v[j]);
-        }
+                    for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4v, v[j][t]), __builtin_bit_cast(short4v, p[j][n][q]), o[n][t], 0, 0, 0);
+        if (i + 2 < count) refill_v();
+    };
+    if (count > 0) {
+        fetch_ids(0);
+        refill_k(0);
+        refill_v();
     }
+    int i = 0;
+    for (; i < plain; i += 2) round(i, std::true_type{});
+    for (; i < count; i += 2) round(i, std::false_type{});
     // tile by tile: the wavefronts' results, then those of the cuts.  A thread has CH elements of a column.
     const int rc = tid >> 4, ch = (tid & 15) * CH;
     const size_t unit = size_t(blockIdx.x) * a.Hkv + kvh;
-    constexpr int PART = 16 * (H + 2);  // floats that a cut leaves per tile: [16][H], [16] maxima, [16] sums
+    constexpr int PART = kPartFloats<H>;
     float* part = a.part + (unit * a.cuts + cut) * (PART * NT);
     float acc[NT][CH], acc_m[NT], acc_l[NT];
 #pragma unroll
@@ -349,66 +413,19 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
             for (int e = 0; e < CH; ++e) acc[n][e] += f * red[w][rc][ch + e];
         }
     }
-    if (n_cuts > 1) {
-        const __amdgpu_buffer_rsrc_t rs = dev_rsrc(part);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (rho0 + n * 16 + rc < R) {
-#pragma unroll
-                for (int e = 0; e < CH; e += 4) {
-                    const floatx4 w = {acc[n][e], acc[n][e + 1], acc[n][e + 2], acc[n][e + 3]};
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4v, w), rs, (n * PART + rc * H + ch + e) * 4, 0, kAuxDev);
-                }
-                if (ch == 0) {
-                    st_agent(part + n * PART + 16 * H + rc, acc_m[n]);
-                    st_agent(part + n * PART + 16 * H + 16 + rc, acc_l[n]);
-                }
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (tid == 0) last = __hip_atomic_fetch_add(&a.arrived[unit], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == uint32_t(n_cuts) - 1;
-        __syncthreads();
-        if (!last) return;
-        const float* first = a.part + unit * a.cuts * (PART * NT);
+    if (uc.n > 1) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             if (rho0 + n * 16 + rc >= R) continue;
-            float mg = -INFINITY, lg = 0.f;
 #pragma unroll
-            for (int e = 0; e < CH; ++e) acc[n][e] = 0.f;
-            constexpr int GROUP = 8;  // cuts whose results are under way together
-            for (int s0 = 0; s0 < n_cuts; s0 += GROUP) {
-                float m[GROUP], l[GROUP];
-                uint4v w[GROUP][CH / 4];
-#pragma unroll
-                for (int g = 0; g < GROUP; ++g) {
-                    const float* from = first + size_t(min(s0 + g, n_cuts - 1)) * (PART * NT) + n * PART;
-                    m[g] = ld_agent(from + 16 * H + rc);
-                    l[g] = ld_agent(from + 16 * H + 16 + rc);
-                    const __amdgpu_buffer_rsrc_t rf = dev_rsrc(from);
-#pragma unroll
-                    for (int e = 0; e < CH / 4; ++e) w[g][e] = __builtin_amdgcn_raw_buffer_load_b128(rf, (rc * H + ch + e * 4) * 4, 0, kAuxDev);
-                }
-                float mnew = mg;
-#pragma unroll
-                for (int g = 0; g < GROUP; ++g) mnew = fmaxf(mnew, m[g]);
-                const float mref = mnew == -INFINITY ? 0.f : mnew, old = __builtin_amdgcn_exp2f(mg - mref);
-                lg *= old;
-#pragma unroll
-                for (int e = 0; e < CH; ++e) acc[n][e] *= old;
-#pragma unroll
-                for (int g = 0; g < GROUP; ++g) {
-                    const float f = s0 + g < n_cuts ? __builtin_amdgcn_exp2f(m[g] - mref) : 0.f;
-                    lg += f * l[g];
-#pragma unroll
-                    for (int e = 0; e < CH; ++e) acc[n][e] += f * __uint_as_float(w[g][e / 4][e % 4]);
-                }
-                mg = mnew;
+            for (int e = 0; e < CH; e += 4)
+                *reinterpret_cast<floatx4*>(part + n * PART + rc * H + ch + e) = floatx4{acc[n][e], acc[n][e + 1], acc[n][e + 2], acc[n][e + 3]};
+            if (ch == 0) {
+                part[n * PART + 16 * H + rc] = acc_m[n];
+                part[n * PART + 16 * H + 16 + rc] = acc_l[n];
             }
-            acc_l[n] = lg;
         }
+        return;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -419,6 +436,77 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
 #pragma unroll
         for (int e = 0; e < CH; ++e) to[e] = static_cast<T>(acc[n][e] * inv);
     }
+}
+
+// Adds up what the cuts of a unit left.  One workgroup: four columns of a tile, sixteen threads each, four times over: every fourth cut, of which the
+// results of four are under way together.  The sums are taken in an order that the number of cuts fixes.
+template <int H, typename T, int NT>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+    constexpr int CH = H / 16, PART = kPartFloats<H>, GROUP = 4;
+    __shared__ float red[4][4][16][CH + 2];
+    const SeqUnit u = find_unit(a, blockIdx.x, a.G, 16 * NT, 1);
+    const int R = u.n_new * a.G, rho0 = u.index * 16 * NT, n = blockIdx.z >> 2;
+    if (u.index < 0 || rho0 + n * 16 + (blockIdx.z & 3) * 4 >= R) return;
+    const UnitCuts uc = cuts_of(a, u, (min(rho0 + 16 * NT, R) - 1) / a.G);
+    if (uc.n == 1) return;
+    const int tid = threadIdx.x, quarter = tid >> 6, at = tid & 15, cl = tid >> 4 & 3, rc = (blockIdx.z & 3) * 4 + cl, ch = at * CH;
+    const int rho = rho0 + n * 16 + rc;
+    const float* first = a.part + (size_t(blockIdx.x) * a.Hkv + blockIdx.y) * a.cuts * (PART * NT) + n * PART;
+    float mg = -INFINITY, lg = 0.f, acc[CH];
+#pragma unroll
+    for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+    if (rho < R)
+        for (int s0 = quarter; s0 < uc.n; s0 += 4 * GROUP) {
+            float m[GROUP], l[GROUP];
+            floatx4 w[GROUP][CH / 4];
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                const float* from = first + size_t(min(s0 + 4 * g, uc.n - 1)) * (PART * NT);
+                m[g] = s0 + 4 * g < uc.n ? from[16 * H + rc] : -INFINITY;
+                l[g] = from[16 * H + 16 + rc];
+#pragma unroll
+                for (int e = 0; e < CH / 4; ++e) w[g][e] = *reinterpret_cast<const floatx4*>(from + rc * H + ch + e * 4);
+            }
+            float mnew = mg;
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) mnew = fmaxf(mnew, m[g]);
+            const float mref = mnew == -INFINITY ? 0.f : mnew, old = __builtin_amdgcn_exp2f(mg - mref);
+            lg *= old;
+#pragma unroll
+            for (int e = 0; e < CH; ++e) acc[e] *= old;
+#pragma unroll
+            for (int g = 0; g < GROUP; ++g) {
+                const float f = __builtin_amdgcn_exp2f(m[g] - mref);
+                lg += f * l[g];
+#pragma unroll
+                for (int e = 0; e < CH; ++e) acc[e] += f * w[g][e / 4][e % 4];
+            }
+            mg = mnew;
+        }
+#pragma unroll
+    for (int e = 0; e < CH; ++e) red[quarter][cl][at][e] = acc[e];
+    red[quarter][cl][at][CH] = mg;
+    red[quarter][cl][at][CH + 1] = lg;
+    __syncthreads();
+    const Column c = column_of(a, u, blockIdx.y, rho);
+    if (quarter != 0 || !c.ok) return;
+#pragma unroll
+    for (int q = 1; q < 4; ++q) mg = fmaxf(mg, red[q][cl][at][CH]);
+    const float mref = mg == -INFINITY ? 0.f : mg;
+    lg = 0.f;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float f = __builtin_amdgcn_exp2f(red[q][cl][at][CH] - mref);
+        lg += f * red[q][cl][at][CH + 1];
+#pragma unroll
+        for (int e = 0; e < CH; ++e) acc[e] += f * red[q][cl][at][e];
+    }
+    const float inv = lg == 0.f ? 0.f : 1.0f / lg;
+    T* to = static_cast<T*>(a.out) + int64_t(c.row) * a.o_row + int64_t(c.head) * a.o_head + ch;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) to[e] = static_cast<T>(acc[e] * inv);
 }
 
 }  // namespace card

@@ -78,36 +78,47 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
     return launch_status();
 }
 
-// How the attention of a call is run: tiles of 16 * tiles rows x heads, the pages of a sequence in cuts.
+// How the attention of a call is run: tiles of 16 * tiles rows x heads, the pages of a sequence in cuts; the new tokens stored by the
+// same kernel, or by one in front.
+#ifndef FILL1
+#define FILL1 1024
+#define FILL2 1024
+#define FILL4 512
+#endif
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
-    size_t counter_bytes, bytes;
+    bool fused;
+    size_t bytes;
 };
-constexpr int kAttendFill = 1024;  // workgroups that a call is cut for
-AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b) {
+AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f32) {
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
-    const int64_t new_most = b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows;
-    p.tiles = new_most * G <= 16 ? 1 : 2;
+    const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
+    p.fused = most <= 64;
+    p.tiles = most <= 16 ? 1 : (f32 || most <= 32 || most > 64 ? 2 : 4);
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
-    p.cut_pages = std::max(8, ceil_div(ceil_div(int64_t(p.units) * cfg->n_kv_heads * pages, kAttendFill), 8) * 8);
+    p.cut_pages = std::max(8, ceil_div(ceil_div(int64_t(p.units) * cfg->n_kv_heads * pages, p.tiles == 1 ? FILL1 : p.tiles == 2 ? FILL2 : FILL4), 8) * 8);
     p.cuts = ceil_div(pages, p.cut_pages);
-    if (p.cuts > 1) {
-        const size_t groups = size_t(p.units) * cfg->n_kv_heads;
-        p.counter_bytes = align_up(groups * 4, 1024);
-        p.bytes = p.counter_bytes + groups * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
-    }
+    if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;
 }
 
-template <int H, typename T>
+template <int H, typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-    if (a.k || a.counters)
-        hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
     const dim3 grid(uint32_t(p.units), uint32_t(a.Hkv), uint32_t(p.cuts));
-    if (p.tiles == 1) hipLaunchKernelGGL((k_attend_few<H, T, 1>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_attend_few<H, T, 2>), grid, dim3(256), 0, st, a);
+    if (a.k && p.fused) {
+        hipLaunchKernelGGL((k_attend_few<H, T, NT, true>), grid, dim3(256), 0, st, a);
+    } else {
+        if (a.k)
+            hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
+        hipLaunchKernelGGL((k_attend_few<H, T, NT, false>), grid, dim3(256), 0, st, a);
+    }
+    if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, grid.y, 4 * NT), dim3(256), 0, st, a);
+}
+template <typename T, int NT>
+void attend_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t st) {
+    h == 128 ? attend_launch<128, T, NT>(a, p, st) : attend_launch<64, T, NT>(a, p, st);
 }
 
 }  // namespace
@@ -167,7 +178,8 @@ int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
 }
 
 size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch) {
-    return batch_ok(cfg, batch) && batch->n_rows > 0 ? attend_plan(cfg, batch).bytes : 0;
+    if (!batch_ok(cfg, batch) || batch->n_rows == 0) return 0;
+    return std::max(attend_plan(cfg, batch, false).bytes, attend_plan(cfg, batch, true).bytes);
 }
 
 int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
@@ -182,7 +194,7 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
     if (k && (!rows_ok(k, q->type, 0) || !rows_ok(v, q->type, 0))) return CARD_EINVAL;
     if (mask && (!mask->mask_dev || !mask->mask_base_dev || mask->words < 1 || mask->words > (1 << 25))) return CARD_EINVAL;
-    const AttendPlan plan = attend_plan(cfg, batch);
+    const AttendPlan plan = attend_plan(cfg, batch, q->type == CARD_F32);
     if (plan.bytes > 0 && (!workspace_dev || !aligned16(workspace_dev))) return CARD_EINVAL;
     AttendArgs a = {};
     a.q = q->data;
@@ -218,15 +230,13 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     a.scale = 1.4426950408889634f / sqrtf(float(cfg->head_dim));
     a.cuts = plan.cuts;
     a.cut_pages = plan.cut_pages;
-    if (plan.cuts > 1) {
-        a.counters = plan.units * cfg->n_kv_heads;
-        a.arrived = static_cast<uint32_t*>(workspace_dev);
-        a.part = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + plan.counter_bytes);
-    }
+    a.part = static_cast<float*>(workspace_dev);
     hipStream_t st = as_stream(stream);
-    const bool wide = cfg->head_dim == 128;
-    if (q->type == CARD_F32) wide ? attend_launch<128, float>(a, plan, st) : attend_launch<64, float>(a, plan, st);
-    else wide ? attend_launch<128, __bf16>(a, plan, st) : attend_launch<64, __bf16>(a, plan, st);
+    const int h = cfg->head_dim;
+    if (q->type == CARD_F32) plan.tiles == 1 ? attend_launch<float, 1>(a, plan, h, st) : attend_launch<float, 2>(a, plan, h, st);
+    else if (plan.tiles == 1) attend_launch<__bf16, 1>(a, plan, h, st);
+    else if (plan.tiles == 2) attend_launch<__bf16, 2>(a, plan, h, st);
+    else attend_launch<__bf16, 4>(a, plan, h, st);
     return launch_status();
 }
 
