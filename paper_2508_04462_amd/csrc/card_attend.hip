@@ -7,6 +7,7 @@
 namespace card {
 
 typedef __attribute__((ext_vector_type(2))) unsigned int uint2v;
+typedef __attribute__((address_space(4))) int32_t const_i32;  // memory that no kernel writes meanwhile: scalar loads
 
 struct AttendArgs {
     const void* q;
@@ -39,22 +40,24 @@ __device__ __forceinline__ int32_t seq_start(const AttendArgs& a, int s) {
 }
 __device__ __forceinline__ SeqUnit find_unit(const AttendArgs& a, int unit, int mul, int div, int add) {
     const int lane = threadIdx.x & 63;
-    const auto first = [&](int s) { return int(int64_t(seq_start(a, s)) * mul / div) + add * s; };
-    int lo = 0, hi = a.n_seqs;  // 64 places are looked at at a time: one load up to 64 sequences
-    while (hi - lo > 1) {
+    const auto first = [&](int start, int s) { return int(int64_t(start) * mul / div) + add * s; };
+    int lo = 0, hi = a.n_seqs;
+    while (hi - lo > 64) {  // 64 places are looked at at a time
         const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
-        const int hits = __popcll(__ballot(s < hi && first(s) <= unit));
+        const int hits = __popcll(__ballot(s < hi && first(seq_start(a, min(s, hi - 1)), s) <= unit));
         lo += max(hits - 1, 0) * step;
         hi = min(hi, lo + step);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
+    // the last 64: all that is to be known of each, in one round trip
+    const int s = min(lo + lane, hi - 1), start = seq_start(a, s), end = seq_start(a, s + 1), held = a.ctx[s];
+    const int at = max(__popcll(__ballot(lo + lane < hi && first(start, s) <= unit)) - 1, 0);
     SeqUnit u;
-    u.seq = lo;
-    u.index = unit - first(lo);
-    u.row0 = seq_start(a, lo);
-    u.n_new = max(seq_start(a, lo + 1) - u.row0, 0);
+    u.seq = __builtin_amdgcn_readfirstlane(lo + at);
+    u.row0 = __builtin_amdgcn_readlane(start, at);
+    u.index = unit - first(u.row0, u.seq);
+    u.n_new = max(__builtin_amdgcn_readlane(end, at) - u.row0, 0);
     const int room = a.table_pages * 16;
-    u.ctx = min(max(a.ctx[lo], 0), room);
+    u.ctx = min(max(__builtin_amdgcn_readlane(held, at), 0), room);
     u.len = min(u.ctx + u.n_new, room);
     return u;
 }
@@ -166,39 +169,59 @@ __device__ __forceinline__ uint2v first_of_four(int n) {
 }
 __device__ __forceinline__ uint32_t bf16_bits(__bf16 v) { return __builtin_bit_cast(unsigned short, v); }
 
-// A page that new tokens belong to: their keys and values come from the call's arrays, whoever of the workgroups that read the page stores
-// them in it.  Tokens [own0, own1) are this wavefront's to store.
-template <int H, typename T>
-__device__ __forceinline__ void take_new_tokens(const AttendArgs& a, const SeqUnit& u, int id, int kvh, int slot, int lane, int own0, int own1,
-                                                bf16x8 (&k)[H / 32], uint2v (&v)[H / 16]) {
-    const int col = lane & 15, t0 = slot + (lane >> 4) * 4;
+// The new tokens of a workgroup's pages, from the call's arrays: in LDS for the rounds that need them, K as it lies, V transposed, by place in the
+// cache so that the four tokens of a lane lie together; and in their pages, tokens [own0, own1), which are this workgroup's to store
+// (whoever else reads the page takes them from the arrays, too).
+constexpr int kStage = 64;
+template <int H>
+struct Stage {
+    __bf16 k[kStage][H];
+    __bf16 v[H][kStage + 4];
+};
+// Stores 8 elements of a token, from element c * 8 on.
+template <int H>
+__device__ __forceinline__ void store_token(const AttendArgs& a, const SeqUnit& u, int kvh, int slot, int c, bf16x8 k, bf16x8 v) {
+    const int id = a.tables[int64_t(u.seq) * a.table_pages + (slot >> 4)];
+    if (id < 0 || id >= a.n_pages) return;
     const size_t page = (size_t(id) * a.Hkv + kvh) * (16 * H);
-    const int tok = slot + col;
+    *reinterpret_cast<bf16x8*>(a.kpool + page + (c * 16 + (slot & 15)) * 8) = k;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a.vpool[page + v_page_index(c * 8 + i, slot & 15)] = v[i];
+}
+// What `use` does with 8 elements of each of the new tokens in slots [s0, s1): token, element / 8, key, value.
+template <int H, typename T, typename F>
+__device__ __forceinline__ void each_new_token(const AttendArgs& a, const SeqUnit& u, int kvh, int s0, int s1, F&& use) {
+    const T* k = static_cast<const T*>(a.k) + int64_t(u.row0 - u.ctx) * a.k_row + int64_t(kvh) * a.k_head;
+    const T* v = static_cast<const T*>(a.v) + int64_t(u.row0 - u.ctx) * a.v_row + int64_t(kvh) * a.v_head;
+    for (int e = threadIdx.x; e < (s1 - s0) * (H / 8); e += 256) {
+        const int slot = s0 + e / (H / 8), c = e % (H / 8);
+        const T* pk = k + slot * a.k_row + c * 8;
+        const T* pv = v + slot * a.v_row + c * 8;
+        bf16x8 wk, wv;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            wk[i] = static_cast<__bf16>(pk[i]);
+            wv[i] = static_cast<__bf16>(pv[i]);
+        }
+        use(slot, c, wk, wv);
+    }
+}
+template <int H>
+__device__ __forceinline__ void take_new_tokens(const SeqUnit& u, int slot, int lane, const Stage<H>& sm, bf16x8 (&k)[H / 32], uint2v (&v)[H / 16]) {
+    const int col = lane & 15, kq = lane >> 4, tok = slot + col, t0 = slot + kq * 4;
     const bool fresh = tok >= u.ctx && tok < u.len;
-    const T* p = static_cast<const T*>(a.k) + int64_t(u.row0 + (fresh ? tok - u.ctx : 0)) * a.k_row + int64_t(kvh) * a.k_head + (lane >> 4) * 8;
+    const int row = fresh ? tok - u.ctx : 0;
 #pragma unroll
     for (int st = 0; st < H / 32; ++st) {
-        bf16x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = static_cast<__bf16>(p[st * 32 + e]);
+        const bf16x8 w = *reinterpret_cast<const bf16x8*>(&sm.k[row][st * 32 + kq * 8]);
         k[st] = fresh ? w : k[st];
-        if (fresh && tok >= own0 && tok < own1) *(reinterpret_cast<bf16x8*>(a.kpool + page) + st * 64 + lane) = w;
     }
-    const T* pv[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        pv[e] = static_cast<const T*>(a.v) + int64_t(u.row0 + min(max(t0 + e - u.ctx, 0), u.n_new - 1)) * a.v_row + int64_t(kvh) * a.v_head + col;
     const uint2v below = first_of_four(u.len - t0), old = first_of_four(u.ctx - t0), take = {below[0] & ~old[0], below[1] & ~old[1]};
+    const int at = min(max(t0 - (u.ctx & ~3), 0), kStage);
 #pragma unroll
     for (int i = 0; i < H / 16; ++i) {
-        __bf16 w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = static_cast<__bf16>(pv[e][i * 16]);
-        v[i][0] = (v[i][0] & ~take[0]) | ((bf16_bits(w[0]) | bf16_bits(w[1]) << 16) & take[0]);
-        v[i][1] = (v[i][1] & ~take[1]) | ((bf16_bits(w[2]) | bf16_bits(w[3]) << 16) & take[1]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (t0 + e >= own0 && t0 + e < min(own1, u.len)) a.vpool[page + (i >> 1) * 512 + lane * 8 + (i & 1) * 4 + e] = w[e];
+        const uint2v w = *reinterpret_cast<const uint2v*>(&sm.v[i * 16 + col][at]);
+        v[i] = (v[i] & ~take) | (w & take);
     }
 }
 
@@ -226,7 +249,11 @@ constexpr int kPartFloats = 16 * (H + 2);
 template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4 ? 2 : 1)) void k_attend_few(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, LD = H + 4, CH = H / 16;
-    __shared__ __align__(16) float red[4][16][LD];
+    __shared__ union __align__(16) {
+        Stage<H> stage;
+        float red[4][16][LD];
+    } sm;
+    auto& red = sm.red;
     __shared__ float red_m[4][16], red_l[4][16];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, kvh = blockIdx.y, cut = blockIdx.z;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -240,6 +267,14 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
     const int all_see = a.mask ? min(base, u.len) : min(u.ctx + m_first + 1, u.len);  // slots below are seen by every row
     const int own0 = u.ctx + (rho0 + a.G - 1) / a.G, own1 = u.ctx + m_last + 1;  // the tokens whose first head is among the rows
+    bool fresh = NEW && p1 * 16 > u.ctx;  // new tokens among this cut's
+    if (NEW && fresh && u.n_new > kStage) {  // more than max_new said: they go to their pages first (the same values by whoever reads them)
+        each_new_token<H, T>(a, u, kvh, max(u.ctx, cut * uc.pages * 16), min(u.len, p1 * 16),
+                             [&](int slot, int c, bf16x8 wk, bf16x8 wv) { store_token<H>(a, u, kvh, slot, c, wk, wv); });
+        __threadfence_block();
+        __syncthreads();
+        fresh = false;
+    }
     Column c[NT];
     bf16x8 qf[NT][NP][ST];
     floatx4 o[NT][HT];
@@ -253,29 +288,30 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
         mx[n] = -INFINITY;
         sum[n] = 0.f;
     }
-    const int32_t* table = a.tables + int64_t(u.seq) * a.table_pages;
-    int ids = 0;  // of this wavefront's pages, 64 at a time, a lane each
-    const auto page_id = [&](int i) { return __builtin_amdgcn_readlane(ids, i & 63); };
+    // page ids are scalar loads, a round ahead: they wait on a counter of their own, not on the pages under way
+    const const_i32* table = reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(a.tables + int64_t(u.seq) * a.table_pages));
     const int count = p0 < p1 ? (p1 - p0 + 3) >> 2 : 0;
-    const auto fetch_ids = [&](int i) { ids = i + lane < count ? table[p0 + 4 * (i + lane)] : -1; };
+    const auto page_id = [&](int i) { return i < count ? table[p0 + 4 * i] : -1; };
     const auto held = [&](int id) { return id >= 0 && id < a.n_pages; };
     // pages that hold no new token and that every row sees whole come first, in pairs: their rounds have no memory access but the
-    // refills, which then stay in flight
-    const int plain_pages = min(NEW ? min(u.ctx, all_see) : all_see, u.len) >> 4;
-    const int plain = (p0 < min(p1, plain_pages) ? (min(p1, plain_pages) - p0 + 3) >> 2 : 0) & ~1;
+    // refills, which then stay in flight (the last round, which has none, goes with the others)
+    const int plain_end = min(p1, min(fresh ? min(u.ctx, all_see) : all_see, u.len) >> 4);
+    const int plain = min(p0 < plain_end ? (plain_end - p0 + 3) >> 2 : 0, count - 2) & ~1;
     bf16x8 k[2][ST];
     uint2v v[2][HT];
-    int id[2];
-    const auto refill_k = [&](int i) {
+    int id[2], next_id[2];
+    const auto refill_k = [&]() {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            id[j] = page_id(i + j);
+            id[j] = next_id[j];
             load_k_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, k[j]);
         }
     };
-    const auto refill_v = [&]() {
+    const auto refill_v = [&](int i) {  // of pages i and i + 1
 #pragma unroll
         for (int j = 0; j < 2; ++j) load_v_page<H>(a, held(id[j]) ? id[j] : 0, kvh, lane, v[j]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) next_id[j] = page_id(i + 2 + j);
     };
     const auto round = [&](int i, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
@@ -289,7 +325,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
         if constexpr (!WHOLE && NEW) {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if (there[j] && slot[j] + 16 > u.ctx) take_new_tokens<H, T>(a, u, id[j], kvh, slot[j], lane, own0, own1, k[j], v[j]);
+                if (fresh && there[j] && slot[j] + 16 > u.ctx) take_new_tokens<H>(u, slot[j], lane, sm.stage, k[j], v[j]);
         }
         floatx4 s[2][NT];
 #pragma unroll
@@ -304,10 +340,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) s[j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][st], qf[n][w][st], s[j][n], 0, 0, 0);
-        if (i + 2 < count) {
-            if (((i + 2) & 63) == 0) fetch_ids(i + 2);
-            refill_k(i + 2);
-        }
+        if (WHOLE || i + 2 < count) refill_k();
         const bool both = there[0] && there[1];
         uint2v p[2][NT][NP];
         float alpha[NT];
@@ -373,16 +406,33 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                 for (int t = 0; t < HT; ++t)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4v, v[j][t]), __builtin_bit_cast(short4v, p[j][n][q]), o[n][t], 0, 0, 0);
-        if (i + 2 < count) refill_v();
+        if (WHOLE || i + 2 < count) refill_v(i + 2);
     };
+    // (loads return in order: the queries, needed in every round, before the first pages)
+    __builtin_amdgcn_sched_barrier(0);
     if (count > 0) {
-        fetch_ids(0);
-        refill_k(0);
-        refill_v();
+        next_id[0] = page_id(0);
+        next_id[1] = page_id(1);
+        refill_k();
+        refill_v(0);
+    }
+    if constexpr (NEW) {
+        if (fresh)
+            each_new_token<H, T>(a, u, kvh, u.ctx, u.len, [&](int slot, int c, bf16x8 wk, bf16x8 wv) {
+                const int t = slot - u.ctx;
+                *reinterpret_cast<bf16x8*>(&sm.stage.k[t][c * 8]) = wk;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sm.stage.v[c * 8 + i][(u.ctx & 3) + t] = wv[i];
+                if (slot >= own0 && slot < own1) store_token<H>(a, u, kvh, slot, c, wk, wv);
+            });
     }
     int i = 0;
-    for (; i < plain; i += 2) round(i, std::true_type{});
-    for (; i < count; i += 2) round(i, std::false_type{});
+    if (count > 0)
+        for (; i < plain; i += 2) round(i, std::true_type{});
+    if (NEW && fresh) __syncthreads();
+    if (count > 0)
+        for (; i < count; i += 2) round(i, std::false_type{});
+    if (NEW && fresh) __syncthreads();  // (the results meet where the new tokens were)
     // tile by tile: the wavefronts' results, then those of the cuts.  A thread has CH elements of a column.
     const int rc = tid >> 4, ch = (tid & 15) * CH;
     const size_t unit = size_t(blockIdx.x) * a.Hkv + kvh;
