@@ -237,6 +237,8 @@ __device__ __forceinline__ UnitCuts cuts_of(const AttendArgs& a, const SeqUnit& 
     return c;
 }
 
+constexpr float kSlack = 8.f;
+
 // Floats that a cut leaves of a tile: [16][H], [16] maxima, [16] sums.
 template <int H>
 constexpr int kPartFloats = 16 * (H + 2);
@@ -245,6 +247,9 @@ constexpr int kPartFloats = 16 * (H + 2);
 // the registers that the matrix instructions take it from.  One workgroup: one cut of the pages of a sequence, for one KV head; its four
 // wavefronts take every fourth page each, two per round, and refill K as soon as the scores are done, V behind P V.  The wavefronts' results
 // meet in LDS, the cuts' in memory, where k_attend_join adds them up.
+// The KV heads of a unit are neighbours in the launch and so go to different compute dies: the dies' shares do not depend on how long which
+// sequence is, and the workgroups of one head, which read the same pages, share an L2 (2000 rows x 4 behind 14000 tokens, 8 KV heads, units as
+// neighbours 700 us, heads 666).
 // NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 5 us.
 template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4 ? 2 : 1)) void k_attend_few(AttendArgs a) {
@@ -255,9 +260,10 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     } sm;
     auto& red = sm.red;
     __shared__ float red_m[4][16], red_l[4][16];
-    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, kvh = blockIdx.y, cut = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, cut = blockIdx.y;
+    const int kvh = blockIdx.x % uint32_t(a.Hkv), at_unit = blockIdx.x / uint32_t(a.Hkv);
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const SeqUnit u = find_unit(a, blockIdx.x, a.G, 16 * NT, 1);
+    const SeqUnit u = find_unit(a, at_unit, a.G, 16 * NT, 1);
     const int R = u.n_new * a.G, rho0 = u.index * 16 * NT;
     if (u.index < 0 || rho0 >= R) return;
     const int m_first = rho0 / a.G, m_last = (min(rho0 + 16 * NT, R) - 1) / a.G;
@@ -343,7 +349,6 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
         if (WHOLE || i + 2 < count) refill_k();
         const bool both = there[0] && there[1];
         uint2v p[2][NT][NP];
-        float alpha[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             if (!WHOLE || !both) {
@@ -360,31 +365,35 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                     for (int e = 0; e < 4; ++e) s[j][n][e] = ok[e] ? s[j][n][e] : -INFINITY;
                 }
             }
-            float pmax = -INFINITY;
+            // The weights are 2^(score - mx) with mx a maximum that is raised only where a score passes it by 2^kSlack: the sums and the
+            // output, which a raise multiplies, are then left alone in nearly every round, and no weight exceeds 2^kSlack.
+            float pmax = s[0][n][0];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[j][n][e] *= a.scale;
-                    pmax = fmaxf(pmax, s[j][n][e]);
-                }
-            const float mnew = fmaxf(mx[n], max_across_rows(pmax)), mref = mnew == -INFINITY ? 0.f : mnew;
-            alpha[n] = __builtin_amdgcn_exp2f(mx[n] - mref);
-            mx[n] = mnew;
-            float psum = 0.f;
+                for (int e = 0; e < 4; ++e) pmax = fmaxf(pmax, s[j][n][e]);
+            if (__ballot(pmax * a.scale > mx[n] + kSlack)) {
+                const float mnew = fmaxf(mx[n], max_across_rows(pmax * a.scale));
+                const float alpha = __builtin_amdgcn_exp2f(mx[n] - (mnew == -INFINITY ? 0.f : mnew));
+                mx[n] = mnew;
+                sum[n] *= alpha;
+#pragma unroll
+                for (int t = 0; t < HT; ++t) o[n][t] *= alpha;
+            }
+            const float mref = mx[n] == -INFINITY ? 0.f : mx[n];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
-                    const float x0 = __builtin_amdgcn_exp2f(s[j][n][e] - mref), x1 = __builtin_amdgcn_exp2f(s[j][n][e + 1] - mref);
-                    psum += x0 + x1;
+                    const float x0 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref));
+                    const float x1 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref));
+                    sum[n] += x0 + x1;  // (of this lane's keys; the four lanes of a column are added up at the end)
                     __bf16 w0[NP], w1[NP];
                     split_parts<NP>(x0, w0);
                     split_parts<NP>(x1, w1);
 #pragma unroll
                     for (int q = 0; q < NP; ++q) p[j][n][q][e / 2] = bf16_bits(w0[q]) | bf16_bits(w1[q]) << 16;
                 }
-            sum[n] = sum[n] * alpha[n] + psum;  // (of this lane's keys; the four lanes of a column are added up at the end)
         }
         if (!WHOLE || !both) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
 #pragma unroll
@@ -394,10 +403,6 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                 for (int t = 0; t < HT; ++t) v[j][t] &= own;
             }
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int t = 0; t < HT; ++t) o[n][t] *= alpha[n];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -435,9 +440,8 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     if (NEW && fresh) __syncthreads();  // (the results meet where the new tokens were)
     // tile by tile: the wavefronts' results, then those of the cuts.  A thread has CH elements of a column.
     const int rc = tid >> 4, ch = (tid & 15) * CH;
-    const size_t unit = size_t(blockIdx.x) * a.Hkv + kvh;
     constexpr int PART = kPartFloats<H>;
-    float* part = a.part + (unit * a.cuts + cut) * (PART * NT);
+    float* part = a.part + (size_t(blockIdx.x) * a.cuts + cut) * (PART * NT);
     float acc[NT][CH], acc_m[NT], acc_l[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -494,14 +498,14 @@ template <int H, typename T, int NT>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     constexpr int CH = H / 16, PART = kPartFloats<H>, GROUP = 4;
     __shared__ float red[4][4][16][CH + 2];
-    const SeqUnit u = find_unit(a, blockIdx.x, a.G, 16 * NT, 1);
-    const int R = u.n_new * a.G, rho0 = u.index * 16 * NT, n = blockIdx.z >> 2;
-    if (u.index < 0 || rho0 + n * 16 + (blockIdx.z & 3) * 4 >= R) return;
+    const SeqUnit u = find_unit(a, blockIdx.x / uint32_t(a.Hkv), a.G, 16 * NT, 1);
+    const int R = u.n_new * a.G, rho0 = u.index * 16 * NT, n = blockIdx.y >> 2;
+    if (u.index < 0 || rho0 + n * 16 + (blockIdx.y & 3) * 4 >= R) return;
     const UnitCuts uc = cuts_of(a, u, (min(rho0 + 16 * NT, R) - 1) / a.G);
     if (uc.n == 1) return;
-    const int tid = threadIdx.x, quarter = tid >> 6, at = tid & 15, cl = tid >> 4 & 3, rc = (blockIdx.z & 3) * 4 + cl, ch = at * CH;
+    const int tid = threadIdx.x, quarter = tid >> 6, at = tid & 15, cl = tid >> 4 & 3, rc = (blockIdx.y & 3) * 4 + cl, ch = at * CH;
     const int rho = rho0 + n * 16 + rc;
-    const float* first = a.part + (size_t(blockIdx.x) * a.Hkv + blockIdx.y) * a.cuts * (PART * NT) + n * PART;
+    const float* first = a.part + size_t(blockIdx.x) * a.cuts * (PART * NT) + n * PART;
     float mg = -INFINITY, lg = 0.f, acc[CH];
 #pragma unroll
     for (int e = 0; e < CH; ++e) acc[e] = 0.f;
@@ -538,7 +542,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     red[quarter][cl][at][CH] = mg;
     red[quarter][cl][at][CH + 1] = lg;
     __syncthreads();
-    const Column c = column_of(a, u, blockIdx.y, rho);
+    const Column c = column_of(a, u, blockIdx.x % uint32_t(a.Hkv), rho);
     if (quarter != 0 || !c.ok) return;
 #pragma unroll
     for (int q = 1; q < 4; ++q) mg = fmaxf(mg, red[q][cl][at][CH]);

@@ -80,11 +80,10 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
 
 // How the attention of a call is run: tiles of 16 * tiles rows x heads, the pages of a sequence in cuts; the new tokens stored by the
 // same kernel, or by one in front.
-#ifndef FILL1
-#define FILL1 1024
-#define FILL2 1024
-#define FILL4 512
-#endif
+// Cuts are made for this many workgroups: of one tile three fit a compute unit and a second round evens out what sequences of
+// different lengths leave (48 texts of 400-4000 tokens: 256 workgroups 107 us, 768 95, 2048 91, 4096 91); of more, whose rounds are longer, one per
+// compute unit (32700 tokens: 128 workgroups 51 us, 256 32, 512 41; 100 tree rows in fp32: 256 14, 1024 19).
+constexpr int attend_fill(int tiles) { return tiles == 1 ? 2048 : 256; }
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
     bool fused;
@@ -98,7 +97,7 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
     p.tiles = most <= 16 ? 1 : (f32 || most <= 32 || most > 64 ? 2 : 4);
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
-    p.cut_pages = std::max(8, ceil_div(ceil_div(int64_t(p.units) * cfg->n_kv_heads * pages, p.tiles == 1 ? FILL1 : p.tiles == 2 ? FILL2 : FILL4), 8) * 8);
+    p.cut_pages = std::max(8, ceil_div(ceil_div(int64_t(p.units) * cfg->n_kv_heads * pages, attend_fill(p.tiles)), 8) * 8);
     p.cuts = ceil_div(pages, p.cut_pages);
     if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;
@@ -106,7 +105,7 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
 
 template <int H, typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
-    const dim3 grid(uint32_t(p.units), uint32_t(a.Hkv), uint32_t(p.cuts));
+    const dim3 grid(uint32_t(p.units) * uint32_t(a.Hkv), uint32_t(p.cuts));
     if (a.k && p.fused) {
         hipLaunchKernelGGL((k_attend_few<H, T, NT, true>), grid, dim3(256), 0, st, a);
     } else {
@@ -114,7 +113,7 @@ void attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
             hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
         hipLaunchKernelGGL((k_attend_few<H, T, NT, false>), grid, dim3(256), 0, st, a);
     }
-    if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, grid.y, 4 * NT), dim3(256), 0, st, a);
+    if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, 4 * NT), dim3(256), 0, st, a);
 }
 template <typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t st) {
@@ -188,7 +187,7 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     if (!batch->k_pages || !batch->v_pages || !batch->block_tables || !batch->ctx_lens || !batch->row_starts) return CARD_EINVAL;
     if (!aligned16(batch->k_pages) || !aligned16(batch->v_pages)) return CARD_EINVAL;
     if (layer < 0 || layer >= cfg->n_layers) return CARD_ERANGE;
-    if (int64_t(batch->n_rows) * cfg->n_q_heads + batch->n_seqs >= (int64_t(1) << 31)) return CARD_ERANGE;
+    if (int64_t(batch->n_rows) * cfg->n_q_heads + int64_t(kStoreUnits) * batch->n_seqs * cfg->n_kv_heads >= (int64_t(1) << 31)) return CARD_ERANGE;
     if (batch->n_rows == 0) return CARD_OK;
     if (!q || !out || (q->type != CARD_BF16 && q->type != CARD_F32)) return CARD_EINVAL;
     if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
