@@ -30,6 +30,8 @@ struct AttendArgs {
     float* part;
 };
 
+__device__ __forceinline__ uint32_t bf16_bits(__bf16 v) { return __builtin_bit_cast(unsigned short, v); }
+
 // The sequence and the part of it that unit number `unit` of a launch is about.  Units are dealt so that no prefix sum is needed:
 // sequence s has the units from floor(start_s * mul / div) + add * s on, which are enough for ceil(new_s * mul / div) + add - 1 of them.
 struct SeqUnit {
@@ -90,20 +92,37 @@ __global__ __launch_bounds__(256) void k_attend_store(AttendArgs a, int h) {
     for (int e = threadIdx.x; e < 4 * h; e += 256) {
         const int j = e % h, t = e / h * 4;
         __bf16* to = a.vpool + base + v_page_index(j, t);
+        __bf16 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = static_cast<__bf16>(v[(row0 + min(max(t + i, t0), t1 - 1)) * a.v_row + j]);
+        if (t >= t0 && t + 4 <= t1) {
+            *reinterpret_cast<uint2v*>(to) = uint2v{bf16_bits(w[0]) | bf16_bits(w[1]) << 16, bf16_bits(w[2]) | bf16_bits(w[3]) << 16};
+            continue;
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (t + i >= t0 && t + i < t1) to[i] = static_cast<__bf16>(v[(row0 + t + i) * a.v_row + j]);
+            if (t + i >= t0 && t + i < t1) to[i] = w[i];
     }
 }
 
-// A float as the sum of N bf16: of one part 8 bits of it, of three all 24.
+// Two floats as sums of N bf16, a pair in each word: of one part 8 bits of them, of three all 24.
 template <int N>
-__device__ __forceinline__ void split_parts(float v, __bf16 (&p)[N]) {
+__device__ __forceinline__ void split_pair(float x0, float x1, uint32_t (&p)[N]) {
+    typedef __attribute__((ext_vector_type(2))) float float2v;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        p[i] = static_cast<__bf16>(v);
-        v -= static_cast<float>(p[i]);
+        p[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((float2v{x0, x1}), bf16x2));
+        if (i + 1 < N) {
+            x0 -= __uint_as_float(p[i] << 16);
+            x1 -= __uint_as_float(p[i] & 0xffff0000u);
+        }
     }
+}
+__device__ __forceinline__ uint32_t pack_pair(float x0, float x1) {
+    uint32_t p[1];
+    split_pair<1>(x0, x1, p);
+    return p[0];
 }
 
 // Which of the four keys from slot on a row sees.  limit: its own slot (causal), or the last one of the sequence.
@@ -138,14 +157,18 @@ template <int H, typename T, int NP>
 __device__ __forceinline__ void load_query(const AttendArgs& a, const Column& c, int kq, bf16x8 (&qf)[NP][H / 32]) {
     const T* p = static_cast<const T*>(a.q) + int64_t(c.row) * a.q_row + int64_t(c.head) * a.q_head + kq * 8;
 #pragma unroll
-    for (int st = 0; st < H / 32; ++st)
+    for (int st = 0; st < H / 32; ++st) {
+        uint4v w[NP];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            __bf16 w[NP];
-            split_parts<NP>(static_cast<float>(p[st * 32 + e]), w);
+        for (int e = 0; e < 4; ++e) {
+            uint32_t pair[NP];
+            split_pair<NP>(static_cast<float>(p[st * 32 + 2 * e]), static_cast<float>(p[st * 32 + 2 * e + 1]), pair);
 #pragma unroll
-            for (int i = 0; i < NP; ++i) qf[i][st][e] = w[i];
+            for (int i = 0; i < NP; ++i) w[i][e] = pair[i];
         }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) qf[i][st] = __builtin_bit_cast(bf16x8, w[i]);
+    }
 }
 template <int H>
 __device__ __forceinline__ void load_k_page(const AttendArgs& a, int id, int kvh, int lane, bf16x8 (&k)[H / 32]) {
@@ -167,7 +190,6 @@ __device__ __forceinline__ void load_v_page(const AttendArgs& a, int id, int kvh
 __device__ __forceinline__ uint2v first_of_four(int n) {
     return uint2v{(n > 0 ? 0xffffu : 0u) | (n > 1 ? 0xffff0000u : 0u), (n > 2 ? 0xffffu : 0u) | (n > 3 ? 0xffff0000u : 0u)};
 }
-__device__ __forceinline__ uint32_t bf16_bits(__bf16 v) { return __builtin_bit_cast(unsigned short, v); }
 
 // The new tokens of a workgroup's pages, from the call's arrays: in LDS for the rounds that need them, K as it lies, V transposed, by place in the
 // cache so that the four tokens of a lane lie together; and in their pages, tokens [own0, own1), which are this workgroup's to store
@@ -271,7 +293,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     if (cut >= uc.n) return;
     const int p0 = cut * uc.pages + wave, p1 = min(uc.all_pages, (cut + 1) * uc.pages);
     const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
-    const int all_see = a.mask ? min(base, u.len) : min(u.ctx + m_first + 1, u.len);  // slots below are seen by every row
+    const int all_see = __builtin_amdgcn_readfirstlane(a.mask ? min(base, u.len) : min(u.ctx + m_first + 1, u.len));  // slots below are seen by every row
     const int own0 = u.ctx + (rho0 + a.G - 1) / a.G, own1 = u.ctx + m_last + 1;  // the tokens whose first head is among the rows
     bool fresh = NEW && p1 * 16 > u.ctx;  // new tokens among this cut's
     if (NEW && fresh && u.n_new > kStage) {  // more than max_new said: they go to their pages first (the same values by whoever reads them)
@@ -388,11 +410,10 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
                     const float x0 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref));
                     const float x1 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref));
                     sum[n] += x0 + x1;  // (of this lane's keys; the four lanes of a column are added up at the end)
-                    __bf16 w0[NP], w1[NP];
-                    split_parts<NP>(x0, w0);
-                    split_parts<NP>(x1, w1);
+                    uint32_t pair[NP];
+                    split_pair<NP>(x0, x1, pair);
 #pragma unroll
-                    for (int q = 0; q < NP; ++q) p[j][n][q][e / 2] = bf16_bits(w0[q]) | bf16_bits(w1[q]) << 16;
+                    for (int q = 0; q < NP; ++q) p[j][n][q][e / 2] = pair[q];
                 }
         }
         if (!WHOLE || !both) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
@@ -489,6 +510,230 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
         T* to = static_cast<T*>(a.out) + int64_t(rcol.row) * a.o_row + int64_t(rcol.head) * a.o_head + ch;
 #pragma unroll
         for (int e = 0; e < CH; ++e) to[e] = static_cast<T>(acc[n][e] * inv);
+    }
+}
+
+// For many rows: 128 rows x heads of a KV head at a time, 32 per wavefront.  Every page is fetched once per workgroup, four pages a step, into
+// LDS: K as it lies, V with two pages side by side, so that 16 bytes of a lane are its operand of a matrix instruction over 32 tokens.  The step
+// behind is under way meanwhile (registers, then the other buffer).  Two workgroups per compute unit, whose matrix instructions, softmax and
+// barriers fall into each other's gaps.  Per 32 tokens a wavefront issues 512 clocks of matrix instructions, about as many of softmax, and takes
+// 16 KiB out of LDS, 128 clocks of it, where four wavefronts issue at once: the three bounds lie close together.
+constexpr int kManyWaves = 4, kManyTiles = 2 * kManyWaves;  // tiles of 16 rows x heads of a workgroup
+template <int H>
+__global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
+    using T = __bf16;
+    constexpr int ST = H / 32, HT = H / 16, UNITS = ST * 64, PAGES = 4;  // UNITS: 16 bytes each of a page of one head
+    constexpr int PER = UNITS * PAGES / 256;                            // of K, and of V, of a thread per step
+    __shared__ uint4v sk[2][PAGES][UNITS], sv[2][PAGES / 2][HT * 64];
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, cut = blockIdx.y;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % uint32_t(a.Hkv);
+    const int at_unit = (gridDim.x - 1 - blockIdx.x) / uint32_t(a.Hkv);  // the last rows, which see most, first
+    const SeqUnit u = find_unit(a, at_unit, a.G, 16 * kManyTiles, 1);
+    const int R = u.n_new * a.G, rho0 = u.index * 16 * kManyTiles;
+    if (u.index < 0 || rho0 >= R) return;
+    const UnitCuts uc = cuts_of(a, u, (min(rho0 + 16 * kManyTiles, R) - 1) / a.G);
+    if (cut >= uc.n) return;
+    const int p0 = __builtin_amdgcn_readfirstlane(cut * uc.pages);
+    const int p1 = __builtin_amdgcn_readfirstlane(min(uc.all_pages, (cut + 1) * uc.pages));
+    const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
+    // the wavefront's rows: slots below all_see are seen by each of them, slots behind last_seen by none
+    const int rw = rho0 + wave * 32;
+    const int all_see = __builtin_amdgcn_readfirstlane(a.mask ? min(base, u.len) : min(u.ctx + rw / a.G + 1, u.len));
+    const int last_seen = __builtin_amdgcn_readfirstlane(rw >= R ? -1 : (a.mask ? u.len : min(u.ctx + (min(rw + 32, R) - 1) / a.G + 1, u.len)) - 1);
+    Column c[2];
+    bf16x8 qf[2][1][ST];
+    floatx4 o[2][HT];
+    floatx4 sum[2];  // of the weights: a product with ones
+    float mx[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        c[n] = column_of(a, u, kvh, rw + n * 16 + col);
+        load_query<H, T, 1>(a, c[n], kq, qf[n]);
+#pragma unroll
+        for (int t = 0; t < HT; ++t) o[n][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        mx[n] = -INFINITY;
+        sum[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const const_i32* table = reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(a.tables + int64_t(u.seq) * a.table_pages));
+    int ids[PAGES];
+    const auto fetch_ids = [&](int p) {
+#pragma unroll
+        for (int j = 0; j < PAGES; ++j) ids[j] = p + j < p1 ? table[p + j] : -1;
+    };
+    // a thread's share of a step: units of K, pairs of units of V (the same lane of a page and of the one behind it)
+    uint4v rk[PER], rv[PER / 2][2];
+    const auto fetch = [&]() {
+        const auto page = [&](const __bf16* pool, int j) {
+            const int id = ids[j];
+            return reinterpret_cast<const uint4v*>(pool + (size_t(id >= 0 && id < a.n_pages ? id : 0) * a.Hkv + kvh) * (16 * H));
+        };
+        const uint4v* pk[PAGES];
+        const uint4v* pv[PAGES];
+#pragma unroll
+        for (int j = 0; j < PAGES; ++j) {
+            pk[j] = page(a.kpool, j);
+            pv[j] = page(a.vpool, j);
+        }
+        if constexpr (UNITS == 256) {
+#pragma unroll
+            for (int j = 0; j < PAGES; ++j) rk[j] = pk[j][tid];
+#pragma unroll
+            for (int j = 0; j < PAGES; ++j) rv[j / 2][j % 2] = pv[j][tid];
+        } else {
+            const bool high = wave >= 2;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) rk[j] = (high ? pk[2 * j + 1] : pk[2 * j])[tid & 127];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) rv[0][j] = (high ? pv[2 + j] : pv[j])[tid & 127];
+        }
+    };
+    const auto pages_held = [&]() {  // of those in ids, a bit each
+        int held = 0;
+#pragma unroll
+        for (int j = 0; j < PAGES; ++j) held |= ids[j] >= 0 && ids[j] < a.n_pages ? 1 << j : 0;
+        return held;
+    };
+    const auto put = [&](int p, int held, uint4v (&tk)[PAGES][UNITS], uint4v (&tv)[PAGES / 2][HT * 64]) {  // what was fetched for the step from page p on
+        const bool ragged = held != (1 << PAGES) - 1 || (p + PAGES) * 16 > u.len;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) tk[(j * 256 + tid) / UNITS][(j * 256 + tid) % UNITS] = rk[j];
+#pragma unroll
+        for (int j = 0; j < PER / 2; ++j) {
+            const int pair = (j * 256 + tid) / UNITS, unit = (j * 256 + tid) % UNITS;
+            uint4v w0 = rv[j][0], w1 = rv[j][1];
+            if (ragged) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
+                const int slot = (p + 2 * pair) * 16 + ((unit & 63) >> 4) * 4;
+                const uint2v m0 = first_of_four(held & (1 << (2 * pair)) ? u.len - slot : 0);
+                const uint2v m1 = first_of_four(held & (2 << (2 * pair)) ? u.len - slot - 16 : 0);
+                w0 &= uint4v{m0[0], m0[1], m0[0], m0[1]};
+                w1 &= uint4v{m1[0], m1[1], m1[0], m1[1]};
+            }
+            const int at = (unit >> 6) * 128 + (unit & 63);
+            tv[pair][at] = uint4v{w0[0], w0[1], w1[0], w1[1]};
+            tv[pair][at + 64] = uint4v{w0[2], w0[3], w1[2], w1[3]};
+        }
+    };
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, uint4v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    // Two pages: scores, weights, output.  Operands are taken out of LDS a phase ahead: V before the scores, the next K before P V.
+    bf16x8 k[2][ST];
+    const auto take_k = [&](const uint4v* k0, const uint4v* k1) {
+#pragma unroll
+        for (int st = 0; st < ST; ++st) {
+            k[0][st] = __builtin_bit_cast(bf16x8, k0[st * 64 + lane]);
+            k[1][st] = __builtin_bit_cast(bf16x8, k1[st * 64 + lane]);
+        }
+    };
+    const auto two_pages = [&](int slot0, int held, const uint4v* tv, auto&& take_next) {
+        bf16x8 v[HT];
+#pragma unroll
+        for (int t = 0; t < HT; ++t) v[t] = __builtin_bit_cast(bf16x8, tv[t * 64 + lane]);
+        __builtin_amdgcn_sched_barrier(0);
+        floatx4 s[2][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s[j][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < ST; ++st)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) s[j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][st], qf[n][0][st], s[j][n], 0, 0, 0);
+        const bool whole = held == 3 && slot0 + 32 <= all_see;
+        uint4v w[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            if (!whole) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    bool ok[4];
+                    seen_keys(a, c[n].row, base, held & (1 << j) ? c[n].limit : -1, slot0 + j * 16 + kq * 4, ok);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[j][n][e] = ok[e] ? s[j][n][e] : -INFINITY;
+                }
+            }
+            float pmax = s[0][n][0];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pmax = fmaxf(pmax, s[j][n][e]);
+            if (__ballot(pmax * a.scale > mx[n] + kSlack)) {
+                const float mnew = fmaxf(mx[n], max_across_rows(pmax * a.scale));
+                const float alpha = __builtin_amdgcn_exp2f(mx[n] - (mnew == -INFINITY ? 0.f : mnew));
+                mx[n] = mnew;
+                sum[n] *= alpha;
+#pragma unroll
+                for (int t = 0; t < HT; ++t) o[n][t] *= alpha;
+            }
+        }
+        take_next();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const float mref = mx[n] == -INFINITY ? 0.f : mx[n];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; e += 2)
+                    w[n][j * 2 + e / 2] = pack_pair(__builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref)),
+                                                    __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref)));
+            sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w[n]), sum[n], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < HT; ++t)
+                o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], __builtin_bit_cast(bf16x8, w[n]), o[n][t], 0, 0, 0);
+        }
+    };
+    fetch_ids(p0);
+    fetch();
+    int held = pages_held();
+    put(p0, held, sk[0], sv[0]);
+    fetch_ids(p0 + PAGES);
+    __syncthreads();
+    // a step: the pages from p on lie in buffer B, those behind them go to the other one
+    const auto step = [&](int p, auto B) {
+        constexpr int buf = decltype(B)::value;
+        const bool more = p + PAGES < p1;
+        if (more) fetch();
+        if (p * 16 <= last_seen) {
+            take_k(sk[buf][0], sk[buf][1]);
+            two_pages(p * 16, held & 3, sv[buf][0], [&]() { take_k(sk[buf][2], sk[buf][3]); });
+            two_pages(p * 16 + 32, held >> 2, sv[buf][1], []() {});
+        }
+        if (more) {
+            held = pages_held();
+            put(p + PAGES, held, sk[buf ^ 1], sv[buf ^ 1]);
+            fetch_ids(p + 2 * PAGES);
+        }
+        __syncthreads();
+    };
+    for (int p = p0; p < p1; p += 2 * PAGES) {
+        step(p, std::integral_constant<int, 0>{});
+        if (p + PAGES >= p1) break;
+        step(p + PAGES, std::integral_constant<int, 1>{});
+    }
+    float* part = a.part + ((size_t(at_unit) * a.Hkv + kvh) * a.cuts + cut) * (kPartFloats<H> * kManyTiles) + wave * 2 * kPartFloats<H>;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        if (!c[n].ok) continue;
+        const float l = sum[n][0];
+        if (uc.n > 1) {
+            float* to = part + n * kPartFloats<H>;
+#pragma unroll
+            for (int t = 0; t < HT; ++t) *reinterpret_cast<floatx4*>(to + col * H + t * 16 + kq * 4) = o[n][t];
+            if (kq == 0) {
+                to[16 * H + col] = mx[n];
+                to[16 * H + 16 + col] = l;
+            }
+            continue;
+        }
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        T* to = static_cast<T*>(a.out) + int64_t(c[n].row) * a.o_row + int64_t(c[n].head) * a.o_head + kq * 4;
+#pragma unroll
+        for (int t = 0; t < HT; ++t) {
+            const floatx4 v = o[n][t] * inv;
+            *reinterpret_cast<uint2v*>(to + t * 16) = uint2v{pack_pair(v[0], v[1]), pack_pair(v[2], v[3])};
+        }
     }
 }
 

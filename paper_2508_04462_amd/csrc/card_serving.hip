@@ -83,7 +83,7 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
 // Cuts are made for this many workgroups: of one tile three fit a compute unit and a second round evens out what sequences of
 // different lengths leave (48 texts of 400-4000 tokens: 256 workgroups 107 us, 768 95, 2048 91, 4096 91); of more, whose rounds are longer, one per
 // compute unit (32700 tokens: 128 workgroups 51 us, 256 32, 512 41; 100 tree rows in fp32: 256 14, 1024 19).
-constexpr int attend_fill(int tiles) { return tiles == 1 ? 2048 : 256; }
+constexpr int attend_fill(int tiles) { return tiles == 1 ? 2048 : (tiles == kManyTiles ? 512 : 256); }
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
     bool fused;
@@ -94,10 +94,12 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
     const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
     p.fused = most <= 64;
-    p.tiles = most <= 16 ? 1 : (f32 || most <= 32 || most > 64 ? 2 : 4);
+    p.tiles = most <= 16 ? 1 : (f32 || most <= 32 ? 2 : (most <= 64 ? 4 : kManyTiles));
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
-    p.cut_pages = std::max(8, ceil_div(ceil_div(int64_t(p.units) * cfg->n_kv_heads * pages, attend_fill(p.tiles)), 8) * 8);
+    const int64_t groups = int64_t(p.units - b->n_seqs + 1) * cfg->n_kv_heads;  // (of the units, about one per sequence has no rows)
+    const int fill = attend_fill(p.tiles);
+    p.cut_pages = groups * 4 > fill * 3 ? pages : std::max(8, ceil_div(ceil_div(groups * pages, fill), 8) * 8);
     p.cuts = ceil_div(pages, p.cut_pages);
     if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;
@@ -106,13 +108,11 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
 template <int H, typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
     const dim3 grid(uint32_t(p.units) * uint32_t(a.Hkv), uint32_t(p.cuts));
-    if (a.k && p.fused) {
-        hipLaunchKernelGGL((k_attend_few<H, T, NT, true>), grid, dim3(256), 0, st, a);
-    } else {
-        if (a.k)
-            hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
-        hipLaunchKernelGGL((k_attend_few<H, T, NT, false>), grid, dim3(256), 0, st, a);
-    }
+    if (a.k && !p.fused)
+        hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
+    if constexpr (NT == kManyTiles) hipLaunchKernelGGL(k_attend_many<H>, grid, dim3(256), 0, st, a);
+    else if (a.k && p.fused) hipLaunchKernelGGL((k_attend_few<H, T, NT, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_attend_few<H, T, NT, false>), grid, dim3(256), 0, st, a);
     if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, 4 * NT), dim3(256), 0, st, a);
 }
 template <typename T, int NT>
@@ -235,7 +235,8 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     if (q->type == CARD_F32) plan.tiles == 1 ? attend_launch<float, 1>(a, plan, h, st) : attend_launch<float, 2>(a, plan, h, st);
     else if (plan.tiles == 1) attend_launch<__bf16, 1>(a, plan, h, st);
     else if (plan.tiles == 2) attend_launch<__bf16, 2>(a, plan, h, st);
-    else attend_launch<__bf16, 4>(a, plan, h, st);
+    else if (plan.tiles == 4) attend_launch<__bf16, 4>(a, plan, h, st);
+    else attend_launch<__bf16, kManyTiles>(a, plan, h, st);
     return launch_status();
 }
 
