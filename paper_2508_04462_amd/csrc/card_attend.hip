@@ -513,18 +513,19 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4
     }
 }
 
-// For many rows: 128 rows x heads of a KV head at a time, 32 per wavefront.  Every page is fetched once per workgroup, four pages a step, into
-// LDS: K as it lies, V with two pages side by side, so that 16 bytes of a lane are its operand of a matrix instruction over 32 tokens.  The step
-// behind is under way meanwhile (registers, then the other buffer).  Two workgroups per compute unit, whose matrix instructions, softmax and
-// barriers fall into each other's gaps.  Per 32 tokens a wavefront issues 512 clocks of matrix instructions, about as many of softmax, and takes
-// 16 KiB out of LDS, 128 clocks of it, where four wavefronts issue at once: the three bounds lie close together.
+// For many rows: 128 rows x heads of a KV head at a time, 32 per wavefront, two pages per round.  Every page is fetched once per workgroup and goes
+// through LDS: K as it lies, V with the two pages side by side, so that 16 bytes of a lane are its operand of a matrix instruction over 32
+// tokens.  A round's phases depend on each other, and a compute unit holds two workgroups, so the rounds overlap: while the
+// weights of round i are taken (vector units), the matrix units make the scores of round i + 1; the pages of round i + 2 go to LDS, those of
+// i + 3 are on their way to registers.  Three buffers, one barrier per round.  Per round a wavefront issues 544 clocks of matrix instructions
+// and about 430 of softmax.
 constexpr int kManyWaves = 4, kManyTiles = 2 * kManyWaves;  // tiles of 16 rows x heads of a workgroup
 template <int H>
 __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
     using T = __bf16;
-    constexpr int ST = H / 32, HT = H / 16, UNITS = ST * 64, PAGES = 4;  // UNITS: 16 bytes each of a page of one head
-    constexpr int PER = UNITS * PAGES / 256;                            // of K, and of V, of a thread per step
-    __shared__ uint4v sk[2][PAGES][UNITS], sv[2][PAGES / 2][HT * 64];
+    constexpr int ST = H / 32, HT = H / 16, UNITS = ST * 64;  // UNITS: 16 bytes each of a page of one head
+    constexpr int PER = UNITS * 2 / 256;                      // of K, and of V, of a thread per round
+    __shared__ uint4v sk[3][2][UNITS], sv[3][HT * 64];
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, cut = blockIdx.y;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % uint32_t(a.Hkv);
@@ -537,10 +538,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
     const int p0 = __builtin_amdgcn_readfirstlane(cut * uc.pages);
     const int p1 = __builtin_amdgcn_readfirstlane(min(uc.all_pages, (cut + 1) * uc.pages));
     const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
-    // the wavefront's rows: slots below all_see are seen by each of them, slots behind last_seen by none
+    // the wavefront's rows: slots below all_see are seen by each of them
     const int rw = rho0 + wave * 32;
-    const int all_see = __builtin_amdgcn_readfirstlane(a.mask ? min(base, u.len) : min(u.ctx + rw / a.G + 1, u.len));
-    const int last_seen = __builtin_amdgcn_readfirstlane(rw >= R ? -1 : (a.mask ? u.len : min(u.ctx + (min(rw + 32, R) - 1) / a.G + 1, u.len)) - 1);
+    const int all_see = __builtin_amdgcn_readfirstlane(a.mask ? min(base, u.len) : min(u.ctx + min(rw, R - 1) / a.G + 1, u.len));
     Column c[2];
     bf16x8 qf[2][1][ST];
     floatx4 o[2][HT];
@@ -555,81 +555,73 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
         mx[n] = -INFINITY;
         sum[n] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const const_i32* table = reinterpret_cast<const const_i32*>(reinterpret_cast<uintptr_t>(a.tables + int64_t(u.seq) * a.table_pages));
-    int ids[PAGES];
-    const auto fetch_ids = [&](int p) {
-#pragma unroll
-        for (int j = 0; j < PAGES; ++j) ids[j] = p + j < p1 ? table[p + j] : -1;
-    };
-    // a thread's share of a step: units of K, pairs of units of V (the same lane of a page and of the one behind it)
-    uint4v rk[PER], rv[PER / 2][2];
-    const auto fetch = [&]() {
-        const auto page = [&](const __bf16* pool, int j) {
-            const int id = ids[j];
-            return reinterpret_cast<const uint4v*>(pool + (size_t(id >= 0 && id < a.n_pages ? id : 0) * a.Hkv + kvh) * (16 * H));
-        };
-        const uint4v* pk[PAGES];
-        const uint4v* pv[PAGES];
-#pragma unroll
-        for (int j = 0; j < PAGES; ++j) {
-            pk[j] = page(a.kpool, j);
-            pv[j] = page(a.vpool, j);
+    const int32_t* table = a.tables + int64_t(u.seq) * a.table_pages;
+    // page ids, a lane each: 64 in use, the next 64 under way
+    int ids = p0 + lane < p1 ? table[p0 + lane] : -1, ids_next = p0 + 64 + lane < p1 ? table[p0 + 64 + lane] : -1;
+    const int rounds = (p1 - p0 + 1) >> 1;
+    const auto held_bit = [&](int id) { return id >= 0 && id < a.n_pages ? 1 : 0; };
+    // a thread's share of a round's pages: the same units of both, or (half as many units) one of either
+    uint4v rk[PER], rv[PER];
+    int got = 0;  // which of the fetched pages are there, a bit each
+    const auto fetch = [&](int i) {
+        if (i > 0 && (i & 31) == 0) {
+            ids = ids_next;
+            ids_next = p0 + 2 * i + 64 + lane < p1 ? table[p0 + 2 * i + 64 + lane] : -1;
         }
-        if constexpr (UNITS == 256) {
-#pragma unroll
-            for (int j = 0; j < PAGES; ++j) rk[j] = pk[j][tid];
-#pragma unroll
-            for (int j = 0; j < PAGES; ++j) rv[j / 2][j % 2] = pv[j][tid];
+        const int id0 = __builtin_amdgcn_readlane(ids, 2 * i & 63), id1 = __builtin_amdgcn_readlane(ids, (2 * i + 1) & 63);
+        got = held_bit(id0) | held_bit(id1) << 1;
+        const size_t at0 = (size_t(got & 1 ? id0 : 0) * a.Hkv + kvh) * (16 * H), at1 = (size_t(got & 2 ? id1 : 0) * a.Hkv + kvh) * (16 * H);
+        if constexpr (PER == 2) {
+            rk[0] = reinterpret_cast<const uint4v*>(a.kpool + at0)[tid];
+            rk[1] = reinterpret_cast<const uint4v*>(a.kpool + at1)[tid];
+            rv[0] = reinterpret_cast<const uint4v*>(a.vpool + at0)[tid];
+            rv[1] = reinterpret_cast<const uint4v*>(a.vpool + at1)[tid];
         } else {
-            const bool high = wave >= 2;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) rk[j] = (high ? pk[2 * j + 1] : pk[2 * j])[tid & 127];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) rv[0][j] = (high ? pv[2 + j] : pv[j])[tid & 127];
+            const size_t at = wave >= 2 ? at1 : at0;
+            rk[0] = reinterpret_cast<const uint4v*>(a.kpool + at)[tid & 127];
+            rv[0] = reinterpret_cast<const uint4v*>(a.vpool + at)[tid & 127];
         }
     };
-    const auto pages_held = [&]() {  // of those in ids, a bit each
-        int held = 0;
-#pragma unroll
-        for (int j = 0; j < PAGES; ++j) held |= ids[j] >= 0 && ids[j] < a.n_pages ? 1 << j : 0;
-        return held;
-    };
-    const auto put = [&](int p, int held, uint4v (&tk)[PAGES][UNITS], uint4v (&tv)[PAGES / 2][HT * 64]) {  // what was fetched for the step from page p on
-        const bool ragged = held != (1 << PAGES) - 1 || (p + PAGES) * 16 > u.len;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) tk[(j * 256 + tid) / UNITS][(j * 256 + tid) % UNITS] = rk[j];
-#pragma unroll
-        for (int j = 0; j < PER / 2; ++j) {
-            const int pair = (j * 256 + tid) / UNITS, unit = (j * 256 + tid) % UNITS;
-            uint4v w0 = rv[j][0], w1 = rv[j][1];
-            if (ragged) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
-                const int slot = (p + 2 * pair) * 16 + ((unit & 63) >> 4) * 4;
-                const uint2v m0 = first_of_four(held & (1 << (2 * pair)) ? u.len - slot : 0);
-                const uint2v m1 = first_of_four(held & (2 << (2 * pair)) ? u.len - slot - 16 : 0);
+    // What was fetched for round i goes to buffer b.  Slots that are not the sequence's may hold anything: not multiplied, not even by zero.
+    const auto put = [&](int i, int b) {
+        const int slot0 = (p0 + 2 * i) * 16;
+        const bool ragged = got != 3 || slot0 + 32 > u.len;
+        if constexpr (PER == 2) {
+            sk[b][0][tid] = rk[0];
+            sk[b][1][tid] = rk[1];
+            uint4v w0 = rv[0], w1 = rv[1];
+            if (ragged) {
+                const int slot = slot0 + ((tid & 63) >> 4) * 4;
+                const uint2v m0 = first_of_four(got & 1 ? u.len - slot : 0), m1 = first_of_four(got & 2 ? u.len - slot - 16 : 0);
                 w0 &= uint4v{m0[0], m0[1], m0[0], m0[1]};
                 w1 &= uint4v{m1[0], m1[1], m1[0], m1[1]};
             }
-            const int at = (unit >> 6) * 128 + (unit & 63);
-            tv[pair][at] = uint4v{w0[0], w0[1], w1[0], w1[1]};
-            tv[pair][at + 64] = uint4v{w0[2], w0[3], w1[2], w1[3]};
+            const int at = (tid >> 6) * 128 + (tid & 63);
+            sv[b][at] = uint4v{w0[0], w0[1], w1[0], w1[1]};
+            sv[b][at + 64] = uint4v{w0[2], w0[3], w1[2], w1[3]};
+        } else {
+            const int page = wave >> 1, unit = tid & 127;
+            sk[b][page][unit] = rk[0];
+            uint4v w = rv[0];
+            if (ragged) {
+                const uint2v m = first_of_four(got & (1 << page) ? u.len - slot0 - page * 16 - ((unit & 63) >> 4) * 4 : 0);
+                w &= uint4v{m[0], m[1], m[0], m[1]};
+            }
+            uint2v* to = reinterpret_cast<uint2v*>(&sv[b][(unit >> 6) * 128 + (unit & 63)]) + page;
+            to[0] = uint2v{w[0], w[1]};
+            to[128] = uint2v{w[2], w[3]};
         }
     };
     const bf16x8 ones = __builtin_bit_cast(bf16x8, uint4v{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-    // Two pages: scores, weights, output.  Operands are taken out of LDS a phase ahead: V before the scores, the next K before P V.
     bf16x8 k[2][ST];
-    const auto take_k = [&](const uint4v* k0, const uint4v* k1) {
+    const auto take_k = [&](int b) {
 #pragma unroll
         for (int st = 0; st < ST; ++st) {
-            k[0][st] = __builtin_bit_cast(bf16x8, k0[st * 64 + lane]);
-            k[1][st] = __builtin_bit_cast(bf16x8, k1[st * 64 + lane]);
+            k[0][st] = __builtin_bit_cast(bf16x8, sk[b][0][st * 64 + lane]);
+            k[1][st] = __builtin_bit_cast(bf16x8, sk[b][1][st * 64 + lane]);
         }
     };
-    const auto two_pages = [&](int slot0, int held, const uint4v* tv, auto&& take_next) {
-        bf16x8 v[HT];
-#pragma unroll
-        for (int t = 0; t < HT; ++t) v[t] = __builtin_bit_cast(bf16x8, tv[t * 64 + lane]);
-        __builtin_amdgcn_sched_barrier(0);
-        floatx4 s[2][2];
+    const auto make_scores = [&](floatx4 (&s)[2][2]) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -640,11 +632,29 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int n = 0; n < 2; ++n) s[j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][st], qf[n][0][st], s[j][n], 0, 0, 0);
-        const bool whole = held == 3 && slot0 + 32 <= all_see;
-        uint4v w[2];
+    };
+    int held, held_next;  // of the pages of this round, of the next one
+    floatx4 s[2][2];
+    fetch(0);
+    held = got;
+    put(0, 0);
+    fetch(1);  // (pages behind the last one: not there)
+    held_next = got;
+    put(1, 1);
+    fetch(2);
+    __syncthreads();
+    take_k(0);
+    make_scores(s);
+    take_k(1);
+    int b = 0;
+    for (int i = 0; i < rounds; ++i) {
+        const int slot0 = (p0 + 2 * i) * 16, b1 = b == 2 ? 0 : b + 1, b2 = b1 == 2 ? 0 : b1 + 1;
+        put(i + 2, b2);  // (read last before the barrier of the round before)
+        const int held_2 = got;
+        fetch(i + 3);
+        if (held != 3 || slot0 + 32 > all_see) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            if (!whole) {
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     bool ok[4];
@@ -652,14 +662,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[j][n][e] = ok[e] ? s[j][n][e] : -INFINITY;
                 }
-            }
-            float pmax = s[0][n][0];
+        }
+        float pmax[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            pmax[n] = s[0][n][0];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pmax = fmaxf(pmax, s[j][n][e]);
-            if (__ballot(pmax * a.scale > mx[n] + kSlack)) {
-                const float mnew = fmaxf(mx[n], max_across_rows(pmax * a.scale));
+                for (int e = 0; e < 4; ++e) pmax[n] = fmaxf(pmax[n], s[j][n][e]);
+            pmax[n] *= a.scale;
+        }
+        if (__ballot(pmax[0] > mx[0] + kSlack || pmax[1] > mx[1] + kSlack)) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const float mnew = fmaxf(mx[n], max_across_rows(pmax[n]));
                 const float alpha = __builtin_amdgcn_exp2f(mx[n] - (mnew == -INFINITY ? 0.f : mnew));
                 mx[n] = mnew;
                 sum[n] *= alpha;
@@ -667,8 +684,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
                 for (int t = 0; t < HT; ++t) o[n][t] *= alpha;
             }
         }
-        take_next();
-        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 v[HT];
+#pragma unroll
+        for (int t = 0; t < HT; ++t) v[t] = __builtin_bit_cast(bf16x8, sv[b][t * 64 + lane]);
+        floatx4 s1[2][2];
+        make_scores(s1);  // of the next round (behind the last one: of nothing, and not used)
+        uint4v w[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const float mref = mx[n] == -INFINITY ? 0.f : mx[n];
@@ -678,39 +699,29 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
                 for (int e = 0; e < 4; e += 2)
                     w[n][j * 2 + e / 2] = pack_pair(__builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref)),
                                                     __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref)));
-            sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w[n]), sum[n], 0, 0, 0);
+        }
 #pragma unroll
-            for (int t = 0; t < HT; ++t)
+        for (int g = 0; g < 4 * ST; ++g) {  // a matrix instruction, four of the softmax's
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x400, 1, 0);
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w[n]), sum[n], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < HT; ++t)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
                 o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], __builtin_bit_cast(bf16x8, w[n]), o[n][t], 0, 0, 0);
-        }
-    };
-    fetch_ids(p0);
-    fetch();
-    int held = pages_held();
-    put(p0, held, sk[0], sv[0]);
-    fetch_ids(p0 + PAGES);
-    __syncthreads();
-    // a step: the pages from p on lie in buffer B, those behind them go to the other one
-    const auto step = [&](int p, auto B) {
-        constexpr int buf = decltype(B)::value;
-        const bool more = p + PAGES < p1;
-        if (more) fetch();
-        if (p * 16 <= last_seen) {
-            take_k(sk[buf][0], sk[buf][1]);
-            two_pages(p * 16, held & 3, sv[buf][0], [&]() { take_k(sk[buf][2], sk[buf][3]); });
-            two_pages(p * 16 + 32, held >> 2, sv[buf][1], []() {});
-        }
-        if (more) {
-            held = pages_held();
-            put(p + PAGES, held, sk[buf ^ 1], sv[buf ^ 1]);
-            fetch_ids(p + 2 * PAGES);
-        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) s[j][n] = s1[j][n];
+        held = held_next;
+        held_next = held_2;
         __syncthreads();
-    };
-    for (int p = p0; p < p1; p += 2 * PAGES) {
-        step(p, std::integral_constant<int, 0>{});
-        if (p + PAGES >= p1) break;
-        step(p + PAGES, std::integral_constant<int, 1>{});
+        b = b1;
+        take_k(b2);
     }
     float* part = a.part + ((size_t(at_unit) * a.Hkv + kvh) * a.cuts + cut) * (kPartFloats<H> * kManyTiles) + wave * 2 * kPartFloats<H>;
 #pragma unroll
@@ -731,8 +742,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
         T* to = static_cast<T*>(a.out) + int64_t(c[n].row) * a.o_row + int64_t(c[n].head) * a.o_head + kq * 4;
 #pragma unroll
         for (int t = 0; t < HT; ++t) {
-            const floatx4 v = o[n][t] * inv;
-            *reinterpret_cast<uint2v*>(to + t * 16) = uint2v{pack_pair(v[0], v[1]), pack_pair(v[2], v[3])};
+            const floatx4 x = o[n][t] * inv;
+            *reinterpret_cast<uint2v*>(to + t * 16) = uint2v{pack_pair(x[0], x[1]), pack_pair(x[2], x[3])};
         }
     }
 }
