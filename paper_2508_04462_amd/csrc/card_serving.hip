@@ -67,6 +67,12 @@ bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
            b->max_new >= 0 && b->max_len >= 0;
 }
 
+template <int ROUND>
+void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
+    if (h == 128) hipLaunchKernelGGL((k_kv_move_slots<128, ROUND>), grid, dim3(384), 0, st, a);
+    else hipLaunchKernelGGL((k_kv_move_slots<64, ROUND>), grid, dim3(192), 0, st, a);
+}
+
 // How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more.
 int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(1024, rows)); }
 size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
@@ -161,17 +167,26 @@ int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
         if (src_host[i] < 0 || src_host[i] >= slots || dst_host[i] < 0 || dst_host[i] >= slots) return CARD_ERANGE;
         if (written.has(src_host[i]) || !written.add(dst_host[i])) return CARD_EINVAL;
     }
+    bool apart = true;  // no move writes what another one reads: they need no order
+    for (int i = 0; i < n; ++i) apart = apart && !written.has(src_host[i]);
     MoveArgs a = {};
     a.kpool = static_cast<__bf16*>(kv->k_pages);
     a.vpool = static_cast<__bf16*>(kv->v_pages);
     a.layer_elems = layer_elems(cfg, kv->n_pages);
     a.n_kv_heads = cfg->n_kv_heads;
-    a.head_dim = cfg->head_dim;
-    for (int i = 0; i < n; i += kMoveSlots) {
-        a.n = std::min(n - i, kMoveSlots);
-        std::copy(src_host + i, src_host + i + a.n, a.src);
-        std::copy(dst_host + i, dst_host + i + a.n, a.dst);
-        hipLaunchKernelGGL(k_kv_move_slots, dim3(uint32_t(cfg->n_kv_heads), uint32_t(cfg->n_layers)), dim3(128), 0, as_stream(stream), a);
+    for (int i = 0; i < n;) {
+        for (a.n = 0; i < n && a.n < kMoveSlots; ++a.n) {
+            const int32_t* d = dst_host + i;
+            const bool four = i + 4 <= n && d[1] == d[0] + 1 && d[2] == d[0] + 2 && d[3] == d[0] + 3;
+            a.src[a.n] = src_host[i];
+            a.dst[a.n] = four && (d[0] - a.n) % 4 != 0 ? -1 : d[0];
+            i += a.dst[a.n] >= 0;
+        }
+        const bool few = apart || a.n <= 3 * kMoveApart;
+        a.part = apart ? kMoveApart : kMoveSlots;
+        const dim3 grid(uint32_t(cfg->n_kv_heads), uint32_t(cfg->n_layers), uint32_t(ceil_div(a.n, a.part)));
+        if (few) move_launch<kMoveApart>(a, cfg->head_dim, grid, as_stream(stream));
+        else move_launch<kMoveRound>(a, cfg->head_dim, grid, as_stream(stream));
     }
     return launch_status();
 }
