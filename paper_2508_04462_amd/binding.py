@@ -380,21 +380,25 @@ def card_kv_move_slots(cfg, kv: CardKV, src_slots, dst_slots, stream=None) -> in
     return lib.card_kv_move_slots(C.byref(cfg), C.byref(kv), len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
 
 
-_TYPES = {"torch.bfloat16": CARD_BF16, "torch.float32": CARD_F32}
+_TYPES = {}
 
 
 def _type(t) -> int:
     """A tensor's card_type; -1, which every entry point refuses, for types that there are none for."""
-    return _TYPES.get(str(t.dtype), -1)
+    got = _TYPES.get(t.dtype)
+    if got is None:
+        got = _TYPES[t.dtype] = {"torch.bfloat16": CARD_BF16, "torch.float32": CARD_F32}.get(str(t.dtype), -1)
+    return got
 
 
 def card_rows(t) -> CardRows:
     """A tensor [rows][heads][head_dim] as card_kv_attend takes it; its last dimension has to be contiguous."""
     rows, heads, h = t.shape
-    if t.stride(2) != 1:
+    row, head, one = t.stride()
+    if one != 1:
         raise ValueError("the elements of a head have to lie side by side")
     # (the stride of a dimension of one says nothing)
-    return CardRows(t.data_ptr(), _type(t), t.stride(0) if rows > 1 else heads * h, t.stride(1) if heads > 1 else h)
+    return CardRows(t.data_ptr(), _type(t), row if rows > 1 else heads * h, head if heads > 1 else h)
 
 
 def card_kv_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:

@@ -68,28 +68,47 @@ struct RowSums {
         t += b.t;
     }
 };
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+    const int i = int(__float_as_uint(v));
+    return fmaxf(v, __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false))));
+}
+__device__ __forceinline__ float sum_of_lanes(float v) {
+    return sum_across_rows(dpp_add<0x140>(dpp_add<0x141>(dpp_add<0x4E>(dpp_add<0xB1>(v)))));
+}
 __device__ __forceinline__ RowSums join_lanes(RowSums r, float c) {
-    for (int d = 1; d < 64; d <<= 1) r.join(RowSums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.t, d)}, c);
-    return r;
+    r.raise(max_across_rows(dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(r.m))))), c);
+    return RowSums{r.m, sum_of_lanes(r.s), sum_of_lanes(r.t)};
 }
 
-// The largest keys that a wavefront has been offered, in order: lane i holds the i-th of them, `least` is number top - 1.  Keys are
-// a logit in the upper half, the complement of its token in the lower one: unique, and equal logits order by token.
-// An offer costs a comparison and a ballot; a key that enters, about 100 clocks.  Of n keys in random order top * ln(n / top) enter.
+// The largest keys that a wavefront has been offered, in order: lane i holds the i-th of them, a key that is not above `least` does not
+// enter.  Keys are a logit in the upper half, the complement of its token in the lower one: unique, and equal logits order by token.
+// An offer costs a comparison and a ballot; a key that enters, about 80 clocks.  Of n keys in random order top * ln(n / top) enter an empty list;
+// floor(), on the first ones, keeps nearly all out that will not stay.
 __device__ __forceinline__ unsigned long long lane_key(unsigned long long v, int lane) {
     return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v)), lane))) |
            (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v >> 32)), lane))) << 32);
 }
 struct TopList {
-    unsigned long long best = 0ull, least = 0ull;
+    unsigned long long best = 0ull, least = 0ull, bottom = 0ull;
+    // upper: the upper half of the largest key that this lane is about to offer.  At least `top` keys reach the top-th largest of the lanes'.
+    __device__ __forceinline__ void floor(uint32_t upper, int top) {
+        uint32_t t = 0u;
+        for (int bit = 31; bit >= 8; --bit)  // (to 24 bits, rounded down)
+            if (__popcll(__ballot(upper >= (t | 1u << bit))) >= top) t |= 1u << bit;
+        if (t > 0u) least = bottom = (static_cast<unsigned long long>(t) << 32) - 1ull;
+    }
     __device__ __forceinline__ void offer(unsigned long long key, int top, int lane) {
         unsigned long long in = __ballot(key > least);
         while (in) {
             const unsigned long long k = lane_key(key, __ffsll(in) - 1);
             const int at = __popcll(__ballot(best > k));
-            const unsigned long long up = __shfl_up(best, 1);
+            const int lo = int(uint32_t(best)), hi = int(uint32_t(best >> 32));  // one lane up
+            const unsigned long long up = uint64_t(uint32_t(__builtin_amdgcn_update_dpp(lo, lo, 0x138, 0xf, 0xf, false))) |
+                                          (uint64_t(uint32_t(__builtin_amdgcn_update_dpp(hi, hi, 0x138, 0xf, 0xf, false))) << 32);
             best = lane < at ? best : (lane == at ? k : up);
-            least = lane_key(best, top - 1);
+            const unsigned long long last = lane_key(best, top - 1);
+            least = last > bottom ? last : bottom;
             in &= in - 1;
             in &= __ballot(key > least);
         }
@@ -203,6 +222,7 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
         for (int u = 0; u < kLpVecs; ++u)
 #pragma unroll
             for (int e = 0; e < VN; ++e) r.add(x[u][e], c);
+        if (a.top > 0 && list.bottom == 0ull && !__ballot(list.best != 0ull)) list.floor(float_key(all + 0.f), a.top);
         // (tokens of later turns are larger: an equal logit does not enter; inside a turn it may)
         if (a.top > 0 && __ballot(float_key(all + 0.f) > uint32_t(list.least >> 32))) {
 #pragma unroll
@@ -235,8 +255,11 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs_join(LogprobArgs a) {
         r.join(RowSums{v[0], v[1], v[2]}, c);
     }
     TopList list;
-    for (int i = tid - lane; i < n; i += kLpThreads)
-        list.offer(i + lane < n ? a.part_keys[size_t(row) * n + i + lane] : 0ull, a.top, lane);
+    for (int i = tid - lane; i < n; i += kLpThreads) {
+        const unsigned long long key = i + lane < n ? a.part_keys[size_t(row) * n + i + lane] : 0ull;
+        if (i == tid - lane) list.floor(uint32_t(key >> 32), a.top);
+        list.offer(key, a.top, lane);
+    }
     r = join_waves(sm, r, list, a.top, c);
     finish_row<T>(a, sm, r, row);
 }
