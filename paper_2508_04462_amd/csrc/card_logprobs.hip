@@ -84,7 +84,7 @@ __device__ __forceinline__ RowSums join_lanes(RowSums r, float c) {
 // The largest keys that a wavefront has been offered, in order: lane i holds the i-th of them, a key that is not above `least` does not
 // enter.  Keys are a logit in the upper half, the complement of its token in the lower one: unique, and equal logits order by token.
 // An offer costs a comparison and a ballot; a key that enters, about 80 clocks.  Of n keys in random order top * ln(n / top) enter an empty list;
-// floor(), on the first ones, keeps nearly all out that will not stay.
+// floor(), on the first ones, keeps nearly all out that will not stay, and so does what the other wavefronts of the row have found.
 __device__ __forceinline__ unsigned long long lane_key(unsigned long long v, int lane) {
     return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v)), lane))) |
            (uint64_t(uint32_t(__builtin_amdgcn_readlane(int(uint32_t(v >> 32)), lane))) << 32);
@@ -96,7 +96,11 @@ struct TopList {
         uint32_t t = 0u;
         for (int bit = 31; bit >= 8; --bit)  // (to 24 bits, rounded down)
             if (__popcll(__ballot(upper >= (t | 1u << bit))) >= top) t |= 1u << bit;
-        if (t > 0u) least = bottom = (static_cast<unsigned long long>(t) << 32) - 1ull;
+        if (t > 0u) at_least((static_cast<unsigned long long>(t) << 32) - 1ull);
+    }
+    __device__ __forceinline__ void at_least(unsigned long long key) {
+        if (key > bottom) bottom = key;
+        if (bottom > least) least = bottom;
     }
     __device__ __forceinline__ void offer(unsigned long long key, int top, int lane) {
         unsigned long long in = __ballot(key > least);
@@ -119,8 +123,15 @@ __device__ __forceinline__ unsigned long long logit_key(float x, int token) {
     return x == -INFINITY ? 0ull : (uint64_t(float_key(x + 0.f)) << 32) | (0xffffffffu - uint32_t(token));
 }
 
+// The logit of a key; -inf of none, or of one below all logits'.
+__device__ __forceinline__ float key_logit(unsigned long long key) {
+    const uint32_t f = uint32_t(key >> 32);
+    return f <= 0x007fffffu ? -INFINITY : __uint_as_float(f & 0x80000000u ? f ^ 0x80000000u : ~f);
+}
+
 struct LogprobShared {
     float sums[kLpWaves][3];
+    unsigned long long least;  // the largest of the wavefronts' `least`: of their keys, too, `top` are not smaller
     unsigned long long keys[kLpWaves * kMaxTop], out[kMaxTop];
 };
 
@@ -159,10 +170,8 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, const LogprobSh
     if (tid < a.top) {
         const unsigned long long key = sm.out[tid];
         const bool none = is_void || key == 0ull;
-        const uint32_t f = uint32_t(key >> 32);
-        const float v = __uint_as_float(f & 0x80000000u ? f ^ 0x80000000u : ~f);
         a.top_tokens[int64_t(row) * a.top + tid] = none ? -1 : int(0xffffffffu - uint32_t(key));
-        a.top_logprobs[int64_t(row) * a.top + tid] = none ? (is_void ? NAN : -INFINITY) : logprob(v);
+        a.top_logprobs[int64_t(row) * a.top + tid] = none ? (is_void ? NAN : -INFINITY) : logprob(key_logit(key));
     }
     if (tid == 64) {  // (another wavefront than the one above)
         if (a.tokens) {
@@ -188,6 +197,8 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
     const int n_units = (lead + a.vocab + VN - 1) / VN, end = min(n_units, (part + 1) * a.part_vecs);
     RowSums r = {kLowest, 0.f, 0.f};
     TopList list;
+    if (tid == 0) sm.least = 0ull;
+    __syncthreads();
     for (int first = part * a.part_vecs + wave * 64 * kLpVecs; first < end; first += kLpThreads * kLpVecs) {
         float x[kLpVecs][VN];
         if (first * VN >= lead && (first + 64 * kLpVecs) * VN <= lead + a.vocab && first + 64 * kLpVecs <= end) {
@@ -222,15 +233,25 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
         for (int u = 0; u < kLpVecs; ++u)
 #pragma unroll
             for (int e = 0; e < VN; ++e) r.add(x[u][e], c);
-        if (a.top > 0 && list.bottom == 0ull && !__ballot(list.best != 0ull)) list.floor(float_key(all + 0.f), a.top);
+        if (a.top == 0) continue;
+        const unsigned long long others = *const_cast<volatile unsigned long long*>(&sm.least);
+        list.at_least(lane_key(others, 0));
+        if (list.bottom == 0ull && !__ballot(list.best != 0ull)) list.floor(float_key(all + 0.f), a.top);
         // (tokens of later turns are larger: an equal logit does not enter; inside a turn it may)
-        if (a.top > 0 && __ballot(float_key(all + 0.f) > uint32_t(list.least >> 32))) {
+        float limit = key_logit(list.least);
+        if (__ballot(all >= limit)) {
+            const unsigned long long before = list.least;
 #pragma unroll
             for (int u = 0; u < kLpVecs; ++u) {
-                if (!__ballot(float_key(most[u] + 0.f) >= uint32_t(list.least >> 32))) continue;
+                if (!__ballot(most[u] >= limit)) continue;
 #pragma unroll
-                for (int e = 0; e < VN; ++e) list.offer(logit_key(x[u][e], (first + u * 64 + lane) * VN + e - lead), a.top, lane);
+                for (int e = 0; e < VN; ++e) {
+                    if (!__ballot(x[u][e] >= limit)) continue;
+                    list.offer(logit_key(x[u][e], (first + u * 64 + lane) * VN + e - lead), a.top, lane);
+                    limit = key_logit(list.least);
+                }
             }
+            if (lane == 0 && list.least > before) atomicMax(&sm.least, list.least);
         }
     }
     r = join_waves(sm, r, list, a.top, c);
@@ -255,6 +276,8 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs_join(LogprobArgs a) {
         r.join(RowSums{v[0], v[1], v[2]}, c);
     }
     TopList list;
+    if (a.top > 0 && a.parts >= a.top)  // of the parts' first keys, the top-th largest
+        list.floor(lane < a.parts ? uint32_t(a.part_keys[size_t(row) * n + lane * a.top] >> 32) : 0u, a.top);
     for (int i = tid - lane; i < n; i += kLpThreads) {
         const unsigned long long key = i + lane < n ? a.part_keys[size_t(row) * n + i + lane] : 0ull;
         if (i == tid - lane) list.floor(uint32_t(key >> 32), a.top);

@@ -73,8 +73,9 @@ void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
     else hipLaunchKernelGGL((k_kv_move_slots<64, ROUND>), grid, dim3(192), 0, st, a);
 }
 
-// How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more.
-int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(1024, rows)); }
+// How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more.  1000 rows of 152064 in bf16,
+// the most probable token: for 512, 768, 1024 or 2048 workgroups 63, 63, 69, 78 us; 300 rows 31, 31, 29, 33; 100 of 128256 in fp32 21, 21, 20, 22.
+int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(768, rows)); }
 size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
 
 template <typename T>
