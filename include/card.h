@@ -545,7 +545,9 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
  *   entropy_dev: fp32 [rows] or NULL: -sum p ln p
  *   top        : 0..32; top_tokens_dev int32 / top_logprobs_dev fp32 [rows][top], most probable first, equal logits by
  *                ascending token id; token -1 and -inf where fewer tokens than that have a logit above -inf
- *   workspace_dev: card_logprobs_workspace_bytes, 16-byte aligned, no preparation; calls that may run at the same time do not share one
+ *   temperature: 1e-30 .. 1e30
+ *   workspace_dev: card_logprobs_workspace_bytes for as many rows or more (NULL where that is 0), 16-byte aligned, no preparation; calls
+ *                that may run at the same time do not share one
  * A logit of -inf is a token without probability (its log probability is -inf).  A row in which no logit is above -inf has log
  * probabilities of -inf and entropy 0; a row with a NaN or +inf is void: NaN, and tokens -1.
  * Errors: CARD_EINVAL, CARD_ERANGE (top), CARD_EDEVICE. */

@@ -257,8 +257,10 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
 }
 
 size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top) {
-    if (rows < 1 || vocab < 1 || top < 0 || top > kMaxTop || logprob_parts(rows, vocab) == 1) return 0;
-    return logprob_sums_bytes(rows, vocab) + size_t(rows) * logprob_parts(rows, vocab) * top * 8;
+    if (rows < 1 || vocab < 1 || top < 0 || top > kMaxTop || ceil_div(vocab, 4096) == 1) return 0;
+    // (r rows have at most r + 767 parts: enough for fewer rows, too)
+    const int64_t parts = std::min(int64_t(rows) * ceil_div(vocab, 4096), int64_t(rows) + 768);
+    return size_t(parts) * (16 + 8 * size_t(top));
 }
 
 int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens_dev,

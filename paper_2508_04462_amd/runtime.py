@@ -90,6 +90,7 @@ class Target:
         assert sorted(order) == list(range(self.n_pages))
         self.block_table = torch.tensor(order, dtype=torch.int32, device=self.device)
         self._prompt_ws, self._prompt_rows = None, 0
+        self._attached = None
         self.out = torch.zeros(4, dtype=torch.int32, device=self.device)
         self.row_argmax = torch.zeros(32, dtype=torch.int32, device=self.device)
         self.cand = torch.zeros(32, dtype=torch.int32, device=self.device)
@@ -142,7 +143,25 @@ class Target:
     def _stream(self) -> int:
         return torch.cuda.current_stream(self.device).cuda_stream
 
+    def attach(self, pool=None, seq: int = 0) -> None:
+        """Steps, prompts and drafts from here on run on sequence `seq` of a SequencePool of the same layers and heads, the positions that they
+        write being among those that it has been extended to; without arguments, on the Target's own pages again."""
+        if pool is not None:
+            a, b = self.cfg, pool.cfg
+            if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.device:
+                raise ValueError("a pool of other layers or heads, or on another device")
+            pool.length(seq)  # (an unknown sequence raises here)
+        self._attached = None if pool is None else (pool, seq)
+
+    def _kv_to_write(self, pending: int, first: int, end: int) -> B.CardKV:
+        """kv() for a call that writes positions [first, end)."""
+        if self._attached is not None and not self._attached[0].writable(self._attached[1], first, end):
+            raise B.CardError(B.CARD_ECAPACITY, "the attached sequence")
+        return self.kv(pending)
+
     def kv(self, pending: int) -> B.CardKV:
+        if self._attached is not None:
+            return self._attached[0].kv(self._attached[1], pending)
         return B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.block_table.data_ptr(),
                         self.n_pages, int(pending))
 
@@ -151,7 +170,7 @@ class Target:
                        cand: Optional[torch.Tensor] = None, sampling: Optional[B.CardSampling] = None) -> int:
         """Enqueue on the current stream; candidates come from `cand` (device int32) or from
         self.cand[:r].  No synchronisation."""
-        kv = self.kv(pending)
+        kv = self._kv_to_write(pending, ctx_len, ctx_len + r)
         cand = self.cand if cand is None else cand
         if sampling is not None:
             return B.card_verify_sampled(self.cfg, self.packed, kv, ctx_len, cand, r, sampling, self.workspace,
@@ -195,7 +214,7 @@ class Target:
         tk = torch.full((n, k), -7, dtype=torch.int32, device=dev)
         tp = torch.zeros((n, k), dtype=torch.float32, device=dev)
         logits = torch.empty((n, self.cfg.vocab), dtype=torch.float32, device=dev) if want_logits else None
-        _check(B.card_draft_level(self.cfg, self.packed, self.kv(-1), ctx_len, rows, n, k, self.workspace, self._stream(),
+        _check(B.card_draft_level(self.cfg, self.packed, self._kv_to_write(-1, first_slot, first_slot + n), ctx_len, rows, n, k, self.workspace, self._stream(),
                                   tk, tp, logits), "card_draft_level")
         torch.cuda.current_stream(dev).synchronize()
         res = {"topk_tokens": tk, "topk_probs": tp}
@@ -252,7 +271,7 @@ class Target:
         pieces = level_pieces(n, lanes)
         if self.level_in_one_pass(n):
             rows = B.CardTreeRows(tok.data_ptr(), pos.data_ptr(), int(first_slot), mask.data_ptr(), words, int(mask_base))
-            _check(B.card_draft_level_wide(self.cfg, self.packed, self.kv(-1), ctx_len, rows, n, pieces[0][1], k, self._level_ws,
+            _check(B.card_draft_level_wide(self.cfg, self.packed, self._kv_to_write(-1, first_slot, first_slot + n), ctx_len, rows, n, pieces[0][1], k, self._level_ws,
                                            cur.cuda_stream, tk, tp), "card_draft_level_wide")
             cur.synchronize()
             return {"topk_tokens": tk, "topk_probs": tp}
@@ -267,7 +286,7 @@ class Target:
                     st.wait_event(ready)
                 rows = B.CardTreeRows(tok[c0:c1].data_ptr(), pos[c0:c1].data_ptr(), int(first_slot) + c0, mask[c0:c1].data_ptr(),
                                       words, int(mask_base))
-                _check(B.card_draft_level_piece(self.cfg, self.packed, self.kv(-1), ctx_len, rows, c1 - c0, int(first_slot),
+                _check(B.card_draft_level_piece(self.cfg, self.packed, self._kv_to_write(-1, first_slot, first_slot + n), ctx_len, rows, c1 - c0, int(first_slot),
                                                 int(first_slot) + n, k, self._lane_ws[lane], st.cuda_stream, tk[c0:c1], tp[c0:c1],
                                                 None), "card_draft_level_piece")
                 ev = torch.cuda.Event()
@@ -293,7 +312,7 @@ class Target:
             # the vocabulary (it is forwarded as the nearest one inside), as a failed step leaves it
             ids = [int(t) for t in tokens]
             up = torch.tensor(ids + [n, -1, 0, n, -1, -1, 0, 0], dtype=torch.int32, device=self.device)
-            _check(B.card_prompt(self.cfg, self.packed, self.kv(-1), 0, up, n, self._prompt_ws, self._prompt_rows, self._stream(),
+            _check(B.card_prompt(self.cfg, self.packed, self._kv_to_write(-1, 0, n), 0, up, n, self._prompt_ws, self._prompt_rows, self._stream(),
                                  up.data_ptr() + 4 * (n + 1)), "card_prompt")
             valid = 0 <= min(ids) and max(ids) < self.cfg.vocab
             self.out.copy_(up[n:n + 4] if valid else up[n + 4:])
@@ -307,6 +326,31 @@ class Target:
         for s in range(0, n, chunk):
             last = self.verify(s, -1, tokens[s:s + chunk])
         return last["row_argmax"][-1]
+
+    def score(self, tokens: Sequence[int], ctx_len: int = 0, top: int = 0, temperature: float = 1.0) -> Dict:
+        """Log probabilities of a text: forwards the tokens behind ctx_len cached ones, in calls of max_r rows, and gives, on the device,
+        "logprob" [n - 1] of tokens[1:], "entropy" [n] of what follows each token and, for top > 0, "top_tokens" and "top_logprobs" [n][top]."""
+        n, dev = len(tokens), self.device
+        if n < 1:
+            raise B.CardError(B.CARD_ERANGE, "score")
+        ids = torch.tensor([int(t) for t in tokens] + [-1], dtype=torch.int32, device=dev)
+        rows = min(n, self.cfg.max_r)
+        logits = torch.empty((rows, self.cfg.vocab), dtype=torch.float32, device=dev)
+        ws = torch.empty(B.card_logprobs_workspace_bytes(rows, self.cfg.vocab, top), dtype=torch.uint8, device=dev)
+        logprob, entropy = (torch.empty(n, dtype=torch.float32, device=dev) for _ in range(2))
+        top_tokens = torch.empty((n, top), dtype=torch.int32, device=dev)
+        top_logprobs = torch.empty((n, top), dtype=torch.float32, device=dev)
+        accepted = []
+        for s in range(0, n, rows):
+            e = min(n, s + rows)
+            _check(self.enqueue_verify(ctx_len + s, -1, e - s, logits, cand=ids[s:e]), "card_verify")
+            accepted.append(self.out[:1].clone())
+            _check(B.card_logprobs(logits[:e - s], ids[s + 1:e + 1], temperature, top, logprob[s:e], entropy[s:e], top_tokens[s:e],
+                                   top_logprobs[s:e], ws, self._stream()), "card_logprobs")
+        if int(torch.cat(accepted).min()) < 0:  # weights not packed, or a token id outside the vocabulary
+            raise B.CardError(B.CARD_EDEVICE, "score")
+        res = {"logprob": logprob[:n - 1], "entropy": entropy}
+        return dict(res, top_tokens=top_tokens, top_logprobs=top_logprobs) if top > 0 else res
 
     def release_prompt_workspace(self) -> None:
         """Give the memory back that prompts work in (8B shape: 0.25 GB; the next prompt takes it again)."""

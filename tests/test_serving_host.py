@@ -113,3 +113,126 @@ def test_reference_sees_what_its_pools_hold():
                 k = kp[1, page, head].view(8, 16, 8)[:, t].reshape(64)
                 v = vp[1, page, head].view(2, 4, 16, 2, 4)[:, t // 4, :, :, t % 4].transpose(1, 2).reshape(64)
                 assert torch.equal(k, want_k[head]) and torch.equal(v, want_v[head])
+
+
+# ---- SequencePool's bookkeeping, its device calls played on the CPU -----------------------------------
+
+
+class PlayedPool(card.SequencePool):
+    """Pages hold one number per slot: what write() put there."""
+
+    def __init__(self, monkeypatch, n_pages, max_ctx):
+        from paper_2508_04462_amd import binding
+
+        monkeypatch.setattr(binding, "card_kv_copy_pages", self._copy)
+        monkeypatch.setattr(binding, "card_kv_move_slots", self._move)
+        self._setup(card.make_cfg(TINY, max_ctx), n_pages, torch.device("cpu"))
+        self.slots = [-1] * (n_pages * 16)
+
+    def _stream(self):
+        return 0
+
+    def _copy(self, cfg, kv, src, dst, stream):
+        assert not set(src) & set(dst) and len(set(dst)) == len(dst)
+        for s, d in zip(src, dst):
+            self.slots[d * 16:d * 16 + 16] = self.slots[s * 16:s * 16 + 16]
+        return card.CARD_OK
+
+    def _move(self, cfg, kv, src, dst, stream):
+        assert all(s not in dst[:i] for i, s in enumerate(src))
+        for s, d in zip(src, dst):
+            self.slots[d] = self.slots[s]
+        return card.CARD_OK
+
+    def write(self, seq, first, values):
+        assert self.writable(seq, first, first + len(values))
+        for i, v in enumerate(values):
+            p = first + i
+            self.slots[self._seqs[seq].pages[p // 16] * 16 + p % 16] = v
+
+    def text(self, seq):
+        s = self._seqs[seq]
+        assert len(s.pages) == (s.length + 15) // 16 and s.table[:len(s.pages)].tolist() == s.pages
+        return [self.slots[s.pages[p // 16] * 16 + p % 16] for p in range(s.length)]
+
+    def check(self):
+        users = [0] * self.n_pages
+        for s in self._seqs.values():
+            for p in s.pages:
+                users[p] += 1
+        assert users == self._users and sorted(self._free) == [p for p in range(self.n_pages) if users[p] == 0]
+
+
+def test_pool_against_lists(monkeypatch):
+    """Random forks, extensions, cuts, compactions and ends of sequences, against plain lists."""
+    import random
+
+    rng = random.Random(5)
+    pool = PlayedPool(monkeypatch, 40, 160)
+    texts, value = {}, 0
+    refused = 0
+    for _ in range(3000):
+        what = rng.choice(["new", "extend", "extend", "extend", "fork", "truncate", "compact", "free"])
+        try:
+            if what == "new":
+                texts[pool.new()] = []
+            elif texts:
+                seq = rng.choice(list(texts))
+                text = texts[seq]
+                if what == "extend":
+                    n = rng.choice([0, 1, 1, 5, 16, 40])
+                    pool.extend(seq, n)
+                    new = list(range(value, value + n))
+                    value += n
+                    pool.write(seq, len(text), new)
+                    texts[seq] = text + new
+                elif what == "fork":
+                    texts[pool.fork(seq)] = list(text)
+                elif what == "truncate":
+                    keep = rng.randint(0, len(text))
+                    pool.truncate(seq, keep)
+                    texts[seq] = text[:keep]
+                elif what == "compact":
+                    first = rng.randint(0, len(text))
+                    kept = sorted(rng.sample(range(first, len(text)), rng.randint(0, len(text) - first)))
+                    pool.compact(seq, first, kept)
+                    texts[seq] = text[:first] + [text[p] for p in kept]
+                elif what == "free" and rng.random() < 0.5:
+                    pool.free(seq)
+                    del texts[seq]
+        except card.CardError as e:
+            assert e.status == card.CARD_ECAPACITY
+            refused += 1
+        pool.check()
+        for seq, text in texts.items():
+            assert pool.text(seq) == text and pool.length(seq) == len(text)
+    assert 10 < refused < 2000
+
+
+def test_pool_refuses(monkeypatch):
+    pool = PlayedPool(monkeypatch, 4, 64)
+    a = pool.new()
+    pool.extend(a, 40)
+    for bad in (lambda: pool.extend(a, -1), lambda: pool.truncate(a, 41), lambda: pool.truncate(a, -1), lambda: pool.compact(a, 41, []),
+                lambda: pool.compact(a, 10, [9]), lambda: pool.compact(a, 10, [12, 12]), lambda: pool.compact(a, 10, [13, 12]),
+                lambda: pool.compact(a, 10, [40])):
+        with pytest.raises(card.CardError) as e:
+            bad()
+        assert e.value.status == card.CARD_ERANGE
+    with pytest.raises(card.CardError) as e:
+        pool.extend(a, 25)  # beyond max_ctx
+    assert e.value.status == card.CARD_ECAPACITY
+    b = pool.fork(a)
+    with pytest.raises(card.CardError):
+        pool.fork(b)  # no page for a copy of the last one
+    assert pool.free_pages == 0 and pool.length(b) == 40
+    assert pool.writable(b, 32, 40) and not pool.writable(b, 31, 40) and not pool.writable(b, 32, 41)
+    with pytest.raises(card.CardError) as e:
+        pool.plan([a], [9])  # rows on a page that the fork holds, too
+    assert e.value.status == card.CARD_EINVAL
+    with pytest.raises(ValueError):
+        pool.plan([], [])
+    pool.free(a)
+    with pytest.raises(KeyError):
+        pool.length(a)
+    assert pool.writable(b, 0, 40)
