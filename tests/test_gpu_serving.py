@@ -116,6 +116,17 @@ def test_attend_under_tree_masks(heads, dtype):
     assert (c.out[::2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (28, 4, 128), (40, 2, 64), (7, 1, 128)], ids=lambda v: "%dx%dx%d" % v)
+def test_attend_of_few_rows_under_tree_masks(heads, dtype):
+    lens = [(70, 3), (16, 1), (0, 2), (530, 3)]
+    Call(Batch(heads, lens, dtype).tree_mask(density=0.5)).run().check()
+    Call(Batch(heads, lens, dtype).tree_mask(words=2, bases=[16, 0, 0, 512])).run().check()
+    c = Call(Batch(heads, lens, dtype).tree_mask(empty=True)).run()
+    c.check()
+    assert (c.out[::2] == 0).all()
+
+
 def test_attend_over_what_the_cache_holds_already():
     b = Batch((10, 2, 128), [(40, 20), (3, 1)], BF16)
     first = Call(b).run()
@@ -130,6 +141,8 @@ def test_attend_over_what_the_cache_holds_already():
 @pytest.mark.parametrize("hints", [(0, 0), (1, 16), (500, 60000)])
 def test_attend_is_right_whatever_the_bounds_say(hints):
     Call(Batch((8, 2, 128), [(700, 40), (33, 1), (0, 3)], BF16, slack=3), max_new=hints[0], max_len=hints[1]).run().check()
+    Call(Batch((4, 2, 64), [(30, 100), (0, 0), (5, 70)], F32), max_new=hints[0], max_len=hints[1]).run().check()
+    Call(Batch((10, 2, 128), [(130, 100), (0, 65)], BF16).tree_mask(), max_new=hints[0], max_len=hints[1]).run().check()
 
 
 def test_attend_of_many_sequences():
@@ -138,6 +151,11 @@ def test_attend_of_many_sequences():
     lens = [(int(c), int(n)) for c, n in zip(torch.randint(0, 90, (150,), generator=g), torch.randint(0, 4, (150,), generator=g))]
     Call(Batch((4, 2, 64), lens, BF16)).run().check()
     Call(Batch((8, 2, 64), [(c, 1) for c, _ in lens[:70]] + [(2000, 1)], F32)).run().check()
+
+
+def test_attend_of_thousands_of_sequences():
+    lens = [(i % 5, 1 if i % 7 else 0) for i in range(4200)]
+    Call(Batch((2, 1, 64), lens, BF16)).run().check()
 
 
 def test_attend_far_apart_scores():
