@@ -229,10 +229,13 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
 #pragma unroll
         for (int u = 1; u < kLpVecs; ++u) all = fmaxf(all, most[u]);
         r.raise(fmaxf(r.m, all), c);
+        RowSums turn = {r.m, 0.f, 0.f};  // (added up on its own: a few roundings of a large sum instead of one per logit)
 #pragma unroll
         for (int u = 0; u < kLpVecs; ++u)
 #pragma unroll
-            for (int e = 0; e < VN; ++e) r.add(x[u][e], c);
+            for (int e = 0; e < VN; ++e) turn.add(x[u][e], c);
+        r.s += turn.s;
+        r.t += turn.t;
         if (a.top == 0) continue;
         const unsigned long long others = *const_cast<volatile unsigned long long*>(&sm.least);
         list.at_least(lane_key(others, 0));
