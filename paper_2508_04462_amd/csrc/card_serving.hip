@@ -116,7 +116,7 @@ template <int H, typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
     const dim3 grid(uint32_t(p.units) * uint32_t(a.Hkv), uint32_t(p.cuts));
     if (a.k && !p.fused)
-        hipLaunchKernelGGL((k_attend_store<T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a, H);
+        hipLaunchKernelGGL((k_attend_store<H, T>), dim3(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv)), dim3(256), 0, st, a);
     if constexpr (NT == kManyTiles) hipLaunchKernelGGL(k_attend_many<H>, grid, dim3(256), 0, st, a);
     else if (a.k && p.fused) hipLaunchKernelGGL((k_attend_few<H, T, NT, true>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((k_attend_few<H, T, NT, false>), grid, dim3(256), 0, st, a);
