@@ -532,7 +532,7 @@ typedef struct card_row_mask {
  * is outside the pool or the table are not stored and not seen.
  * The sums of a row are taken in an order that depends on the sizes of the call (n_rows, n_seqs, max_new, max_len) and
  * on its sequence, not on what runs beside it: the same call gives the same bits.
- * Errors: CARD_EINVAL, CARD_ERANGE (layer; n_rows * n_q_heads >= 2^31), CARD_EDEVICE; nothing is enqueued on error. */
+ * Errors: CARD_EINVAL, CARD_ERANGE (layer; n_rows * n_q_heads / 16 + 2 * n_seqs * n_kv_heads >= 2^24), CARD_EDEVICE; nothing is enqueued on error. */
 size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch);
 int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q,
                    const card_rows* k, const card_rows* v, const card_rows* out, const card_row_mask* mask,
@@ -550,7 +550,7 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
  *                that may run at the same time do not share one
  * A logit of -inf is a token without probability (its log probability is -inf).  A row in which no logit is above -inf has log
  * probabilities of -inf and entropy 0; a row with a NaN or +inf is void: NaN, and tokens -1.
- * Errors: CARD_EINVAL, CARD_ERANGE (top), CARD_EDEVICE. */
+ * Errors: CARD_EINVAL, CARD_ERANGE (top; rows >= 2^24; vocab >= 2^30), CARD_EDEVICE. */
 size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride,
                   const int32_t* tokens_dev, float temperature, int32_t top, float* logprob_dev, float* entropy_dev,

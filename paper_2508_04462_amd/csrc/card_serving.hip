@@ -67,6 +67,12 @@ bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
            b->max_new >= 0 && b->max_len >= 0;
 }
 
+// A launch has less than 2^32 threads in x: 2^24 workgroups of 256.  (units of 16 rows x heads, and of 16 new tokens)
+constexpr int64_t kMostGroups = int64_t(1) << 24;
+bool batch_fits(const card_model_cfg* cfg, const card_kv_batch* b) {
+    return int64_t(b->n_rows) * cfg->n_q_heads / 16 + int64_t(kStoreUnits) * b->n_seqs * cfg->n_kv_heads < kMostGroups;
+}
+
 template <int ROUND>
 void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
     if (h == 128) hipLaunchKernelGGL((k_kv_move_slots<128, ROUND>), grid, dim3(384), 0, st, a);
@@ -76,6 +82,7 @@ void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
 // How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more.  1000 rows of 152064 in bf16,
 // the most probable token: for 512, 768, 1024 or 2048 workgroups 63, 63, 69, 78 us; 300 rows 31, 31, 29, 33; 100 of 128256 in fp32 21, 21, 20, 22.
 int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(768, rows)); }
+constexpr int32_t kMostLogits = 1 << 30;  // of a row: they are counted in 32 bits, with the rest of a 16-byte unit at either end
 size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
 
 template <typename T>
@@ -193,7 +200,7 @@ int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
 }
 
 size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch) {
-    if (!batch_ok(cfg, batch) || batch->n_rows == 0) return 0;
+    if (!batch_ok(cfg, batch) || !batch_fits(cfg, batch) || batch->n_rows == 0) return 0;
     return std::max(attend_plan(cfg, batch, false).bytes, attend_plan(cfg, batch, true).bytes);
 }
 
@@ -203,7 +210,7 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     if (!batch->k_pages || !batch->v_pages || !batch->block_tables || !batch->ctx_lens || !batch->row_starts) return CARD_EINVAL;
     if (!aligned16(batch->k_pages) || !aligned16(batch->v_pages)) return CARD_EINVAL;
     if (layer < 0 || layer >= cfg->n_layers) return CARD_ERANGE;
-    if (int64_t(batch->n_rows) * cfg->n_q_heads + int64_t(kStoreUnits) * batch->n_seqs * cfg->n_kv_heads >= (int64_t(1) << 31)) return CARD_ERANGE;
+    if (!batch_fits(cfg, batch)) return CARD_ERANGE;
     if (batch->n_rows == 0) return CARD_OK;
     if (!q || !out || (q->type != CARD_BF16 && q->type != CARD_F32)) return CARD_EINVAL;
     if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
@@ -268,7 +275,7 @@ int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vo
                   float* top_logprobs_dev, void* workspace_dev, void* stream) {
     if ((type != CARD_BF16 && type != CARD_F32) || rows < 0 || vocab < 1 || row_stride < vocab) return CARD_EINVAL;
     if (!(temperature >= 1e-30f && temperature <= 1e30f)) return CARD_EINVAL;
-    if (top < 0 || top > kMaxTop) return CARD_ERANGE;
+    if (top < 0 || top > kMaxTop || rows >= kMostGroups || vocab >= kMostLogits) return CARD_ERANGE;
     if (rows == 0) return CARD_OK;
     if (!logits_dev || !tokens_dev != !logprob_dev || (top > 0 && (!top_tokens_dev || !top_logprobs_dev))) return CARD_EINVAL;
     if (!tokens_dev && !entropy_dev && top == 0) return CARD_EINVAL;

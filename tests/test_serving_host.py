@@ -68,6 +68,11 @@ def test_attend_refuses_what_it_cannot_run():
         assert call(batch(**change)) == card.CARD_EINVAL, change
     assert call(layer=-1) == call(layer=2) == card.CARD_ERANGE
     assert call(batch(n_rows=1 << 30)) == card.CARD_ERANGE
+    # launches of 2^24 workgroups
+    q_heads, kv_heads = cfg.n_q_heads, cfg.n_kv_heads
+    for big in (batch(n_rows=(1 << 28) // q_heads), batch(n_seqs=(1 << 23) // kv_heads), batch(n_rows=2 ** 31 - 1, n_seqs=2 ** 31 - 1)):
+        assert call(big) == card.CARD_ERANGE and card.card_kv_attend_workspace_bytes(cfg, big) == 0
+    assert card.card_kv_attend_workspace_bytes(cfg, batch(n_rows=(1 << 27) // q_heads, max_len=1)) == 0  # (one cut: none needed)
     assert call(k=None) == call(v=None) == card.CARD_EINVAL  # one without the other
     for name in ("q", "k", "v", "out"):
         assert call(**{name: _rows(card.CARD_F32)}) == card.CARD_EINVAL  # types differ
@@ -96,6 +101,8 @@ def test_logprobs_refuses_what_it_cannot_run():
     assert call(tok=None, lp=None, en=None, top=0) == card.CARD_EINVAL  # nothing asked for
     assert call(torch.zeros(4, 100, dtype=torch.float16)) == call(torch.zeros(4, 100).expand(4, 100)[:, :0]) == card.CARD_EINVAL
     assert call(torch.zeros(1, 100).expand(4, 100)) == card.CARD_EINVAL  # rows over each other
+    raw = lambda rows, vocab: card.lib.card_logprobs(A, card.CARD_F32, rows, vocab, vocab, A, 1.0, 0, A, None, None, None, A, None)  # noqa: E731
+    assert raw(1 << 24, 100) == raw(1, 1 << 30) == card.CARD_ERANGE
     with pytest.raises(ValueError):
         call(torch.zeros(100, 4).T)
 
