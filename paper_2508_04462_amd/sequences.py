@@ -138,8 +138,9 @@ class SequencePool:
                 raise B.CardError(B.CARD_ECAPACITY, "compact")
             self._own(s, shared)
             slot = lambda p: s.pages[p // 16] * 16 + p % 16  # noqa: E731
-            _check(B.card_kv_move_slots(self.cfg, self.kv(seq), [slot(p) for p, _ in moves], [slot(q) for _, q in moves], self._stream()),
-                   "card_kv_move_slots")
+            with torch.cuda.device_of(self.k_pages):
+                _check(B.card_kv_move_slots(self.cfg, self.kv(seq), [slot(p) for p, _ in moves], [slot(q) for _, q in moves], self._stream()),
+                       "card_kv_move_slots")
         self.truncate(seq, first + len(pos))
 
     def writable(self, seq: int, first: int, end: int) -> bool:
@@ -154,8 +155,8 @@ class SequencePool:
 
     def plan(self, seqs: Sequence[int], new: Sequence[int]) -> AttendPlan:
         """A batch: the last new[i] tokens of sequence seqs[i] (extended by them before) are the rows of the calls."""
-        if not seqs or len(seqs) != len(new):
-            raise ValueError("as many numbers of new tokens as sequences, at least one")
+        if not seqs or len(seqs) != len(new) or len(set(seqs)) != len(seqs):
+            raise ValueError("as many numbers of new tokens as sequences, at least one, each sequence once")
         for s, n in zip(seqs, new):
             if n < 0 or not self.writable(s, self.length(s) - n, self.length(s)):
                 raise B.CardError(B.CARD_EINVAL, "plan")
@@ -173,8 +174,9 @@ class SequencePool:
         row_mask = None
         if mask is not None:
             if mask_base is None or mask.dim() != 2 or mask.shape[0] != plan.n_rows or not mask.is_contiguous() or not mask_base.is_contiguous() or \
-                    mask_base.numel() != plan.n_seqs or mask.dtype != torch.int32 or mask_base.dtype != torch.int32:
-                raise ValueError("masks: int32 [rows][words], with mask_base int32 [sequences]")
+                    mask_base.numel() != plan.n_seqs or mask.dtype != torch.int32 or mask_base.dtype != torch.int32 or \
+                    mask.device != self.k_pages.device or mask_base.device != self.k_pages.device:
+                raise ValueError("masks: int32 [rows][words], with mask_base int32 [sequences], on the pool's device")
             row_mask = B.CardRowMask(mask.data_ptr(), mask_base.data_ptr(), mask.shape[1])
         if plan.n_rows == 0:
             return out
@@ -183,7 +185,7 @@ class SequencePool:
         if stream != plan.stream:  # the plan may be dropped before that stream has got to the call
             for t in (plan.ctx_lens, plan.row_starts, plan.tables, plan.workspace):
                 t.record_stream(stream)
-        with torch.cuda.device(self.device):
+        with torch.cuda.device_of(self.k_pages):
             _check(B.card_kv_attend(cfg, plan.batch, layer, *rows, row_mask, plan.workspace, self._stream()), "card_kv_attend")
         return out
 
@@ -213,7 +215,8 @@ class SequencePool:
         src = [s.pages[i] for i in places]
         dst = [self._take() for _ in places]
         kv = B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), None, self.n_pages, -1)
-        _check(B.card_kv_copy_pages(self.cfg, kv, src, dst, self._stream()), "card_kv_copy_pages")
+        with torch.cuda.device_of(self.k_pages):
+            _check(B.card_kv_copy_pages(self.cfg, kv, src, dst, self._stream()), "card_kv_copy_pages")
         for i, d in zip(places, dst):
             self._release(s.pages[i])
             s.pages[i] = d

@@ -1,5 +1,7 @@
 """What card_kv_copy_pages, card_kv_move_slots, card_kv_attend and card_logprobs refuse, and the bookkeeping of SequencePool; no GPU:
 nothing gets as far as a launch."""
+import types
+
 import pytest
 import torch
 
@@ -239,6 +241,15 @@ def test_pool_refuses(monkeypatch):
     assert e.value.status == card.CARD_EINVAL
     with pytest.raises(ValueError):
         pool.plan([], [])
+    with pytest.raises(ValueError):
+        pool.plan([b, b], [2, 1])  # two rows would be one token
+    # a mask in other memory than the pools
+    plan = types.SimpleNamespace(n_rows=2, n_seqs=1)
+    q, kv = torch.zeros(2, TINY.n_q_heads, TINY.head_dim), torch.zeros(2, TINY.n_kv_heads, TINY.head_dim)
+    for mask_dev, base_dev in (("meta", "cpu"), ("cpu", "meta")):
+        with pytest.raises(ValueError):
+            pool.attend(plan, 0, q, kv, kv, mask=torch.zeros(2, 1, dtype=torch.int32, device=mask_dev),
+                        mask_base=torch.zeros(1, dtype=torch.int32, device=base_dev))
     pool.free(a)
     with pytest.raises(KeyError):
         pool.length(a)
