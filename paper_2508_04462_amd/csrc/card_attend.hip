@@ -287,7 +287,7 @@ constexpr int kPartFloats = 16 * (H + 2);
 // neighbours 700 us, heads 666).
 // NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 5 us.
 template <int H, typename T, int NT, bool NEW>
-__global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : (NT * sizeof(T) == 4 ? 2 : 1)) void k_attend_few(AttendArgs a) {
+__global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, LD = H + 4, CH = H / 16;
     __shared__ union __align__(16) {
         Stage<H> stage;

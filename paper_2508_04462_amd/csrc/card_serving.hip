@@ -92,12 +92,18 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
     return launch_status();
 }
 
-// How the attention of a call is run: tiles of 16 * tiles rows x heads, the pages of a sequence in cuts; the new tokens stored by the
-// same kernel, or by one in front.
-// Cuts are made for this many workgroups: of one tile three fit a compute unit and a second round evens out what sequences of
-// different lengths leave (48 texts of 400-4000 tokens: 256 workgroups 107 us, 768 95, 2048 91, 4096 91); of more, whose rounds are longer, one per
-// compute unit (32700 tokens: 128 workgroups 51 us, 256 32, 512 41; 100 tree rows in fp32: 256 14, 1024 19).
-constexpr int attend_fill(int tiles) { return tiles == 1 ? 2048 : (tiles == kManyTiles ? 512 : 256); }
+// How the attention of a call is run.  R: most rows x heads of a KV head that one sequence has; all figures in us, 8 KV heads of 128.
+// Tiles of 16 rows x heads of a workgroup.  R <= 16 one: R = 16 of 16 texts of 300-3000 tokens 25.6, with two 32.5.  R <= 256 two, which
+// read the cache half as often: R = 64 of 48 texts of 400-4000 tokens 115, with one 133, with four (which leave a compute unit one workgroup) 123.  Above,
+// k_attend_many: 16 texts, R = 256: 46 against 71 there, R = 512: 79 against 86; one text of 14000 tokens, R = 512: 54 against 58; 48 texts,
+// R = 384: 246 against 224.  fp32: one, whose three parts of a row fill the registers as more rows would (R = 256: 73, with two 101).
+// The new tokens are stored by the same kernel as long as R <= 256 and they have room in LDS, else by one in front: R = 32 of one text 19.4
+// and 21.6, R = 256 44 and 45 (16 texts 46 and 46), R = 512 82 and 76.
+constexpr int kFewRows = 256;
+// The pages of a sequence are cut to have this many workgroups, two per compute unit, unless there are three quarters of them
+// without (one token each, 256, 512, 768, 2048 workgroups: a text of 14000 tokens 16.0, 18.1, 18.1, 21.5; 48 texts of 400-4000 94.5, 93.9, 93.7, 99.1; R = 128,
+// 14000 tokens, 256, 512, 768: 30, 25, 30; k_attend_many, 250 tokens behind 14000: 101, 82, 95).
+constexpr int kFill = 512;
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
     bool fused;
@@ -107,13 +113,12 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
     const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
-    p.fused = most <= 64;
-    p.tiles = most <= 16 ? 1 : (f32 || most <= 32 ? 2 : (most <= 64 ? 4 : kManyTiles));
+    p.fused = most <= std::min(kFewRows, kStage * G);
+    p.tiles = f32 || most <= 16 ? 1 : (most <= kFewRows ? 2 : kManyTiles);
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
     const int64_t groups = int64_t(p.units - b->n_seqs + 1) * cfg->n_kv_heads;  // (of the units, about one per sequence has no rows)
-    const int fill = attend_fill(p.tiles);
-    p.cut_pages = groups * 4 > fill * 3 ? pages : std::max(8, ceil_div(ceil_div(groups * pages, fill), 8) * 8);
+    p.cut_pages = groups * 4 > kFill * 3 ? pages : std::max(8, ceil_div(ceil_div(groups * pages, kFill), 8) * 8);
     p.cuts = ceil_div(pages, p.cut_pages);
     if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;
@@ -255,10 +260,9 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
     a.part = static_cast<float*>(workspace_dev);
     hipStream_t st = as_stream(stream);
     const int h = cfg->head_dim;
-    if (q->type == CARD_F32) plan.tiles == 1 ? attend_launch<float, 1>(a, plan, h, st) : attend_launch<float, 2>(a, plan, h, st);
+    if (q->type == CARD_F32) attend_launch<float, 1>(a, plan, h, st);
     else if (plan.tiles == 1) attend_launch<__bf16, 1>(a, plan, h, st);
     else if (plan.tiles == 2) attend_launch<__bf16, 2>(a, plan, h, st);
-    else if (plan.tiles == 4) attend_launch<__bf16, 4>(a, plan, h, st);
     else attend_launch<__bf16, kManyTiles>(a, plan, h, st);
     return launch_status();
 }

@@ -127,6 +127,24 @@ def test_attend_of_few_rows_under_tree_masks(heads, dtype):
     assert (c.out[::2] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,new", [((8, 8, 64), (16, 17, 64, 65)), ((4, 2, 64), (8, 9, 63, 64, 65, 128, 129)), ((4, 1, 128), (4, 5, 64, 65, 80)),
+                                       ((8, 1, 64), (2, 3, 32, 33))], ids=lambda v: "_".join("%d" % x for x in v))
+def test_attend_at_the_ends_of_its_variants(heads, new, dtype):
+    """As many rows x heads as one kind of workgroup takes, and one token more; behind texts that are cut and some that are not."""
+    for n in new:
+        lens = [(19, 1), (419, n), (0, n), (3, 0)]
+        Call(Batch(heads, lens, dtype, seed=n)).run().check()
+        masked = Batch(heads, lens, dtype, seed=n).tree_mask(density=0.4)
+        ref = masked.reference()
+        first = Call(masked).run()
+        first.check(ref)
+        again = Call(masked, stored=True)
+        again.k_pool.copy_(first.k_pool)
+        again.v_pool.copy_(first.v_pool)
+        again.run().check(ref)
+
+
 def test_attend_over_what_the_cache_holds_already():
     b = Batch((10, 2, 128), [(40, 20), (3, 1)], BF16)
     first = Call(b).run()
