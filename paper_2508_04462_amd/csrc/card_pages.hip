@@ -36,8 +36,12 @@ struct MoveArgs {
 // instructions: reading ROUND moves before writing any is the order of the list as long as no move reads what an earlier one
 // wrote, and so is reading the next ROUND while these are written.  No barrier, and two rounds under way.  The host puts gaps into the list so that
 // slots that go to four neighbours in a row begin at a multiple of four.
-// 1500 tokens of 32 layers x 8 heads x 128, closing gaps, us: a move at a time, a thread per element, 720; rounds of 64, half as many wavefronts, 189.
-constexpr int kMoveRound = 128, kMoveApart = 32;  // moves of a round, of a workgroup of a list that needs no order
+// 1500 tokens of 32 layers x 8 heads x 128, closing gaps of 600 between them, us: a move at a time, a thread per element, 720; rounds of 96
+// moves 124 (471 MB with the gaps' share of the lines: 3.8 TB/s).
+// Rounds of 32 for short lists, which are a matter of latency: 128 moves in rounds of 32 and of 96 12.6 and 14.6, 192 17.7 and 20.7, 256 21.8 and
+// 20.8, 1500 136 and 124 (of 64, 128 moves: 1500 128, 129; 128 14.8, 18.8); 16 layers, 192 12.4 and 14.6, 256 15.6 and 14.1, 1500 91 and 74.
+constexpr int kMoveRound = 96, kMoveShort = 32;
+constexpr int kMoveApart = kMoveShort;  // moves of a workgroup of a list that needs no order
 template <int H, int ROUND>
 __global__ __launch_bounds__(H / 64 * 192) void k_kv_move_slots(MoveArgs a) {
     typedef __attribute__((ext_vector_type(2))) unsigned int uint2v;

@@ -195,10 +195,9 @@ int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
             a.dst[a.n] = four && (d[0] - a.n) % 4 != 0 ? -1 : d[0];
             i += a.dst[a.n] >= 0;
         }
-        const bool few = apart || a.n <= 3 * kMoveApart;
         a.part = apart ? kMoveApart : kMoveSlots;
         const dim3 grid(uint32_t(cfg->n_kv_heads), uint32_t(cfg->n_layers), uint32_t(ceil_div(a.n, a.part)));
-        if (few) move_launch<kMoveApart>(a, cfg->head_dim, grid, as_stream(stream));
+        if (apart || a.n <= 7 * kMoveShort) move_launch<kMoveShort>(a, cfg->head_dim, grid, as_stream(stream));
         else move_launch<kMoveRound>(a, cfg->head_dim, grid, as_stream(stream));
     }
     return launch_status();

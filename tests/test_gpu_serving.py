@@ -323,6 +323,20 @@ def test_move_slots(heads, layers, pages, kind):
     assert all(torch.equal(p.cpu(), w) for p, w in zip(pools, want))
 
 
+@pytest.mark.parametrize("at", [0, 3])
+def test_move_slots_in_lists_of_every_length(at):
+    """Lengths about those of a round and of a launch, the tokens closing up from place `at` of a page on."""
+    heads, pages = (2, 1, 64), 64
+    for n in (2, 31, 32, 33, 95, 96, 97, 191, 192, 193, 221, 224, 225, 288, 289, 477, 480, 481, 673):
+        g = torch.Generator().manual_seed(n)
+        src = sorted(torch.randperm(pages * PAGE - at - 1, generator=g)[:n].add(at + 1).tolist())
+        dst = [at + i for i in range(n)]
+        pools = _pools(1, pages, heads[1], heads[2], seed=n)
+        want = _move_reference(pools, heads[2], src, dst)
+        _copy(_cfg(heads, 1), pools, src, dst, "card_kv_move_slots")
+        assert all(torch.equal(p.cpu(), w) for p, w in zip(pools, want)), n
+
+
 def test_copies_and_moves_beyond_four_gib():
     heads, pages = (8, 8, 128), (1 << 32) // (8 * 16 * 128 * 2) + 50
     pools = [torch.zeros((2, pages, 8, PAGE * 128), dtype=torch.int16, device="cuda") for _ in range(2)]
