@@ -272,7 +272,7 @@ __device__ __forceinline__ UnitCuts cuts_of(const AttendArgs& a, const SeqUnit& 
     return c;
 }
 
-constexpr float kSlack = 8.f;
+constexpr float kSlack = 8.f;  // (see below; 0, k_attend_many: 507 -> 545 us, three texts of up to 1000 rows x 7 142 -> 167)
 
 // Floats that a cut leaves of a tile: [16][H], [16] maxima, [16] sums.
 template <int H>
@@ -283,9 +283,10 @@ constexpr int kPartFloats = 16 * (H + 2);
 // wavefronts take every fourth page each, two per round, and refill K as soon as the scores are done, V behind P V.  The wavefronts' results
 // meet in LDS, the cuts' in memory, where k_attend_join adds them up.
 // The KV heads of a unit are neighbours in the launch and so go to different compute dies: the dies' shares do not depend on how long which
-// sequence is, and the workgroups of one head, which read the same pages, share an L2 (2000 rows x 4 behind 14000 tokens, 8 KV heads, units as
-// neighbours 700 us, heads 666).
-// NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 5 us.
+// sequence is, and the workgroups of one head, which read the same pages, share an L2 (five rows x 8 behind 32700 tokens 37 us, with the units as neighbours
+// 49; k_attend_many, 2000 rows x 4 behind 14000, 507 and 534; 48 texts of a row each 94.7 and 95.6).
+// NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 2 us.
+// 8 KV heads of 128: 48 texts of 400-4000 tokens, 444 MB, in 90 us (4.9 TB/s); 32700 tokens, 134 MB, in 27.
 template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, LD = H + 4, CH = H / 16;
@@ -531,7 +532,9 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
 // tokens.  A round's phases depend on each other, and a compute unit holds two workgroups, so the rounds overlap: while the
 // weights of round i are taken (vector units), the matrix units make the scores of round i + 1; the pages of round i + 2 go to LDS, those of
 // i + 3 are on their way to registers.  Three buffers, one barrier per round.  Per round a wavefront issues 544 clocks of matrix instructions
-// and about 430 of softmax.
+// and about 430 of softmax, and LDS is busy for 640 clocks of a workgroup; two rounds take 2200.  2000 rows x 4 behind 14000 tokens, 8 KV heads of 128:
+// 492 GFLOP in 500 us, 0.98 PFLOP/s, the matrix units busy 42 % of the time at 2.1 GHz.  64 rows per wavefront, which would halve the LDS reads,
+// leave a compute unit one workgroup and nothing to overlap with: 995 us.
 constexpr int kManyWaves = 4, kManyTiles = 2 * kManyWaves;  // tiles of 16 rows x heads of a workgroup
 template <int H>
 __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
@@ -712,8 +715,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
                 for (int e = 0; e < 4; e += 2)
                     w[j * 2 + e / 2] = pack_pair(__builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref)),
                                                  __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref)));
-            // The products of a tile stay together, in front of the other workgroup's instructions: 2000 rows x 4 behind 14000 tokens 523 us,
-            // without the priority 538, left to the compiler's order 545, with one matrix instruction to three others 546.
+            // The products of a tile stay together, in front of the other workgroup's instructions: 2000 rows x 4 behind 14000 tokens 507 us,
+            // without the priority 521, left to the compiler's order 531.
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w), sum[n], 0, 0, 0);
