@@ -81,7 +81,8 @@ void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
 
 // How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more (one row of 128256 in fp32 in parts
 // of 1024, 4096, 16384 or whole 9.5, 9.2, 12.2, 26 us, eight 10.2, 9.3, 13.0, 28).  1000 rows of 152064 in bf16,
-// the most probable token: for 512, 768, 1024 or 2048 workgroups 63, 63, 69, 78 us; 300 rows 31, 31, 29, 33; 100 of 128256 in fp32 21, 21, 20, 22.
+// the most probable token: for 512, 768, 1024 or 2048 workgroups 54.7, 55.1, 59.4, 67.4 us; 300 rows 28.6, 27.6, 26.8, 30.1; 100 of 128256 in fp32
+// 16.5, 15.8, 15.8, 17.7.
 int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(768, rows)); }
 constexpr int32_t kMostLogits = 1 << 30;  // of a row: they are counted in 32 bits, with the rest of a 16-byte unit at either end
 size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
