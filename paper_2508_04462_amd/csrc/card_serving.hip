@@ -104,8 +104,13 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
 constexpr int kFewRows = 256;
 // The pages of a sequence are cut to have this many workgroups, two per compute unit, unless there are three quarters of them
 // without (one token each, 256, 512, 768, 2048 workgroups: a text of 14000 tokens 16.0, 18.1, 18.1, 21.5; 48 texts of 400-4000 94.5, 93.9, 93.7, 99.1; R = 128,
-// 14000 tokens, 256, 512, 768: 30, 25, 30; k_attend_many, 250 tokens behind 14000: 101, 82, 95).
+// 14000 tokens, 256, 512, 768: 30, 25, 30; k_attend_many, 250 tokens behind 14000: 101, 82, 95).  Counted by rows, so that texts of a few rows, which
+// differ in length, are cut more than that: 48 texts in five cuts 93.9, in two (768 workgroups) 99.6.
 constexpr int kFill = 512;
+// Cuts cost the join, 3 us and a share per workgroup, and gain where a workgroup's pages take longer: not for so many pages.  (uncut and cut; one token each: a
+// text of 500 tokens 7.3 and 8.4, 1000 10.1 and 8.4; 8 texts of 1000 10.2 and 9.8; 30 of 1000 17.3 and 20.2, of 1500 23.0 and 24.4; 100 of 2000 99 and
+// 102; k_attend_many, 100 tokens behind 200 17.0 and 17.0, behind 500 23.6 and 17.2, 500 behind 500 33.3 and 33.8, behind 1500 56 and 42.)
+int64_t pages_uncut(int tiles, int64_t groups) { return tiles == kManyTiles ? 8 + groups / 2 : 32 + groups / 3; }
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
     bool fused;
@@ -119,8 +124,10 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
     p.tiles = f32 || most <= 16 ? 1 : (most <= kFewRows ? 2 : kManyTiles);
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
-    const int64_t groups = int64_t(p.units - b->n_seqs + 1) * cfg->n_kv_heads;  // (of the units, about one per sequence has no rows)
-    p.cut_pages = groups * 4 > kFill * 3 ? pages : std::max(8, ceil_div(ceil_div(groups * pages, kFill), 8) * 8);
+    const int full = p.units - b->n_seqs + 1;  // tiles, if the rows filled them
+    const int64_t groups = int64_t(full) * cfg->n_kv_heads;
+    const bool whole = groups * 4 > kFill * 3 || pages <= pages_uncut(p.tiles, int64_t(std::max(full, b->n_seqs)) * cfg->n_kv_heads);
+    p.cut_pages = whole ? pages : std::max(8, ceil_div(ceil_div(groups * pages, kFill), 8) * 8);
     p.cuts = ceil_div(pages, p.cut_pages);
     if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;

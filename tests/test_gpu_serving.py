@@ -145,6 +145,84 @@ def test_attend_at_the_ends_of_its_variants(heads, new, dtype):
         again.run().check(ref)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,new", [((4, 2, 64), (1, 9, 64, 129)), ((4, 1, 128), (2, 20, 65)), ((20, 2, 128), (1, 3, 30))],
+                         ids=lambda v: "_".join("%d" % x for x in v))
+def test_attend_of_texts_in_cuts(heads, new, dtype):
+    """Texts of which the longest is cut, some ending in its first cuts."""
+    for n in new:
+        lens = [(0, n), (1711, n), (130, 1), (900, 0), (701, n // 2 + 1)]
+        Call(Batch(heads, lens, dtype, seed=n)).run().check()
+        masked = Batch(heads, lens, dtype, seed=n).tree_mask(density=0.4)
+        ref = masked.reference()
+        first = Call(masked).run()
+        first.check(ref)
+        again = Call(masked, stored=True)
+        again.k_pool.copy_(first.k_pool)
+        again.v_pool.copy_(first.v_pool)
+        again.run().check(ref)
+        blind = Call(Batch(heads, lens, dtype, seed=n).tree_mask(empty=True)).run()
+        blind.check()
+        assert (blind.out[::2] == 0).all()
+
+
+def test_one_graph_of_the_operators():
+    """Page copies, moves, attention and log probabilities captured together; the lists stay with the graph.  Replayed with the program's own
+    work between, every replay is the eager calls' result."""
+    import paper_2508_04462_amd as card
+
+    heads, layers = (10, 2, 128), 2
+    cfg = _cfg(heads, layers)
+    b = Batch(heads, [(100, 3), (700, 1), (40, 2)], BF16, layers=layers, seed=8, fill=0.0, spare=4)
+    pages = [p for p in range(b.n_pages) if p not in set(b.tables[b.tables < 2 ** 30].tolist())]
+    first = int(b.tables[0, 0])
+    call = Call(b)
+    logits = (torch.randn((9, 5000), generator=torch.Generator().manual_seed(1)) * 3).cuda()
+    tokens = torch.arange(9, dtype=torch.int32, device="cuda")
+    got = [torch.empty(9, device="cuda"), torch.empty(9, device="cuda"), torch.empty((9, 4), dtype=torch.int32, device="cuda"), torch.empty((9, 4), device="cuda")]
+    ws = torch.empty(card.card_logprobs_workspace_bytes(9, 5000, 4), dtype=torch.uint8, device="cuda")
+
+    def all_of_them():
+        stream = torch.cuda.current_stream().cuda_stream
+        kv = card.CardKV(call.k_pool.data_ptr(), call.v_pool.data_ptr(), None, b.n_pages, -1)
+        src, dst = [first], [pages[0]]
+        assert card.card_kv_copy_pages(cfg, kv, src, dst, stream) == card.CARD_OK
+        src[0] = dst[0] = -1  # read during the call only
+        slots = [first * PAGE + 2, first * PAGE + 5], [first * PAGE, first * PAGE + 1]
+        assert card.card_kv_move_slots(cfg, kv, *slots, stream) == card.CARD_OK
+        call.run()
+        assert card.card_logprobs(logits, tokens, 1.0, 4, *got, ws, stream) == card.CARD_OK
+
+    def state():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (call.out, call.k_pool, call.v_pool, *got)]
+
+    def reset(turn):
+        call.k_pool.copy_(b.k_pool)
+        call.v_pool.copy_(b.v_pool)
+        call.out.fill_(7.0)
+        logits.mul_(1.0 + 0.1 * turn)
+        for t in got:
+            t.zero_()
+
+    graph = torch.cuda.CUDAGraph()
+    all_of_them()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        all_of_them()
+    for turn in range(4):
+        kept = logits.clone()
+        reset(turn)
+        all_of_them()
+        want = state()
+        logits.copy_(kept)
+        reset(turn)
+        graph.replay()
+        for w, g in zip(want, state()):
+            assert torch.equal(w, g)
+        assert int(got[2].min()) >= 0 and not torch.equal(call.k_pool.cpu(), b.k_pool)
+
+
 def test_attend_over_what_the_cache_holds_already():
     b = Batch((10, 2, 128), [(40, 20), (3, 1)], BF16)
     first = Call(b).run()
@@ -444,6 +522,18 @@ def test_logprobs_of_unusual_rows(dtype):
     tokens[9], tokens[10], tokens[11] = -1, vocab, -2 ** 31
     _check_logprobs(x.to(dtype), tokens, 1.0, 8)
     _check_logprobs(x.to(dtype), None, 0.5, 32)
+
+
+def test_logprobs_of_rows_beyond_four_gib():
+    far = (1 << 31) + 24
+    store = torch.empty(far + 1000, dtype=BF16, device="cuda")
+    g = torch.Generator().manual_seed(6)
+    rows = (torch.randn((2, 1000), generator=g) * 3).bfloat16()
+    logits = store.as_strided((2, 1000), (far, 1))
+    logits.copy_(rows)
+    tokens = torch.tensor([5, 999], dtype=torch.int32)
+    got, want = _logprobs(logits, tokens, 1.0, 5), _logprobs(rows.cuda(), tokens, 1.0, 5)
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
 
 
 def test_logprobs_of_a_slice():
