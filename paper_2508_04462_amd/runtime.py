@@ -144,12 +144,14 @@ class Target:
         return torch.cuda.current_stream(self.device).cuda_stream
 
     def attach(self, pool=None, seq: int = 0) -> None:
-        """Steps, prompts and drafts from here on run on sequence `seq` of a SequencePool of the same layers and heads, the positions that they
-        write being among those that it has been extended to; without arguments, on the Target's own pages again."""
+        """Steps, prompts and drafts from here on run on sequence `seq` of a SequencePool of the same layers and heads and at least the Target's
+        max_ctx, the positions that they write being among those that it has been extended to; without arguments, on the Target's own pages again."""
         if pool is not None:
             a, b = self.cfg, pool.cfg
             if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.device:
                 raise ValueError("a pool of other layers or heads, or on another device")
+            if b.max_ctx < a.max_ctx:  # calls may look at as many places of the block table
+                raise ValueError("a pool of shorter sequences")
             pool.length(seq)  # (an unknown sequence raises here)
         self._attached = None if pool is None else (pool, seq)
 

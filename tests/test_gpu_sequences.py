@@ -66,6 +66,18 @@ def test_forks_share_a_prompt_and_go_on_apart(target):
         target.attach()
 
 
+def test_attach_refuses_shorter_tables(target):
+    """A pool whose block tables end before the model's max_ctx."""
+    import paper_2508_04462_amd as card
+
+    pool = card.SequencePool(SHAPE, 8, 496)
+    with pytest.raises(ValueError):
+        target.attach(pool, pool.new())
+    with pytest.raises(KeyError):
+        target.attach(card.SequencePool(SHAPE, 8, 528), 0)
+    target.attach()
+
+
 def _cache(tgt, positions):
     got = [tgt.kv_gather(l, 0, max(positions) + 1) for l in range(SHAPE.n_layers)]
     return [(k[positions], v[positions]) for k, v in got]
