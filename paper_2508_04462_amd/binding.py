@@ -215,7 +215,9 @@ class _Library:
     def __getattr__(self, name):
         if self._cdll is None:
             self._cdll = _declare(_load())
-        return getattr(self._cdll, name)
+        found = getattr(self._cdll, name)
+        setattr(self, name, found)  # (looked up once: a look through here costs 0.4 us)
+        return found
 
 
 lib = _Library()
@@ -223,8 +225,8 @@ lib = _Library()
 
 def _ptr(x) -> Optional[int]:
     """torch tensor -> its data pointer; int / None pass through."""
-    if x is None:
-        return None
+    if x is None or type(x) is int:
+        return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()
     return int(x)
@@ -371,13 +373,13 @@ def card_kv_gather(cfg, kv: CardKV, layer: int, first_slot: int, count: int, k_o
 def card_kv_copy_pages(cfg, kv: CardKV, src_pages, dst_pages, stream=None) -> int:
     if len(src_pages) != len(dst_pages):
         return CARD_EINVAL
-    return lib.card_kv_copy_pages(C.byref(cfg), C.byref(kv), len(src_pages), _i32(src_pages), _i32(dst_pages), _ptr(stream))
+    return lib.card_kv_copy_pages(cfg, kv, len(src_pages), _i32(src_pages), _i32(dst_pages), _ptr(stream))
 
 
 def card_kv_move_slots(cfg, kv: CardKV, src_slots, dst_slots, stream=None) -> int:
     if len(src_slots) != len(dst_slots):
         return CARD_EINVAL
-    return lib.card_kv_move_slots(C.byref(cfg), C.byref(kv), len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
+    return lib.card_kv_move_slots(cfg, kv, len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
 
 
 _TYPES = {}
@@ -385,10 +387,9 @@ _TYPES = {}
 
 def _type(t) -> int:
     """A tensor's card_type; -1, which every entry point refuses, for types that there are none for."""
-    got = _TYPES.get(t.dtype)
-    if got is None:
-        got = _TYPES[t.dtype] = {"torch.bfloat16": CARD_BF16, "torch.float32": CARD_F32}.get(str(t.dtype), -1)
-    return got
+    if t.dtype not in _TYPES:
+        _TYPES[t.dtype] = {"torch.bfloat16": CARD_BF16, "torch.float32": CARD_F32}.get(str(t.dtype), -1)
+    return _TYPES[t.dtype]
 
 
 def card_rows(t) -> CardRows:
@@ -402,14 +403,12 @@ def card_rows(t) -> CardRows:
 
 
 def card_kv_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:
-    return lib.card_kv_attend_workspace_bytes(C.byref(cfg), C.byref(batch))
+    return lib.card_kv_attend_workspace_bytes(cfg, batch)
 
 
 def card_kv_attend(cfg, batch: CardKVBatch, layer: int, q: CardRows, k: Optional[CardRows], v: Optional[CardRows], out: CardRows,
                    mask: Optional[CardRowMask], workspace_dev, stream=None) -> int:
-    return lib.card_kv_attend(C.byref(cfg), C.byref(batch), layer, C.byref(q), None if k is None else C.byref(k),
-                              None if v is None else C.byref(v), C.byref(out), None if mask is None else C.byref(mask),
-                              _ptr(workspace_dev), _ptr(stream))
+    return lib.card_kv_attend(cfg, batch, layer, q, k, v, out, mask, _ptr(workspace_dev), _ptr(stream))
 
 
 def card_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
@@ -420,9 +419,10 @@ def card_logprobs(logits, tokens_dev, temperature: float, top: int, logprob_dev,
                   workspace_dev, stream=None) -> int:
     """logits: a tensor [rows][vocab] whose last dimension is contiguous."""
     rows, vocab = logits.shape
-    if vocab > 1 and logits.stride(1) != 1:
+    row, one = logits.stride()
+    if vocab > 1 and one != 1:
         raise ValueError("the logits of a row have to lie side by side")
-    return lib.card_logprobs(_ptr(logits), _type(logits), rows, vocab, logits.stride(0) if rows > 1 else vocab, _ptr(tokens_dev),
+    return lib.card_logprobs(logits.data_ptr(), _type(logits), rows, vocab, row if rows > 1 else vocab, _ptr(tokens_dev),
                              temperature, top, _ptr(logprob_dev), _ptr(entropy_dev), _ptr(top_tokens_dev), _ptr(top_logprobs_dev),
                              _ptr(workspace_dev), _ptr(stream))
 
