@@ -262,6 +262,23 @@ def test_attend_far_apart_scores():
     Call(b).run().check(ref)
 
 
+@pytest.mark.parametrize("heads,lens", [((8, 2, 128), [(700, 3)]), ((8, 2, 64), [(700, 3)]), ((8, 2, 128), [(300, 150), (2000, 20)])],
+                         ids=["few_128", "few_64", "many"])
+def test_attend_keeps_the_bits_of_fp32(heads, lens):
+    """The mean error, where roundings add as squares.  q and k are N(0, 1): a score and its partial sums have magnitude 1 or less, so the 3 h additions
+    of three-part products leave sqrt(3 h) 2^-24 / sqrt(3); so does a weight, relative to itself, with a handful more from exp2; partial sums of the
+    output are no larger than itself, and n keys leave sqrt(n) 2^-24 / sqrt(3).  q in two parts alone would leave 2^-17 / sqrt(3) = 4.4e-6, beyond the bound."""
+    b = Batch(heads, lens, F32, seed=3)
+    out, mean_abs, score_abs, _, _ = ref = b.reference()
+    c = Call(b).run()
+    c.check(ref)
+    err = c.out.cpu().double() - out
+    n = max(c + m for c, m in lens)
+    bound = 2.0 ** -24 * (math.sqrt(heads[2] + 8) + math.sqrt(n / 3))
+    assert bound < 2.0 ** -17 / math.sqrt(3)
+    assert float(err.square().mean().sqrt()) <= bound * float(out.square().mean().sqrt())
+
+
 def test_attend_with_pages_that_are_not_there():
     """A page id outside the pool, and a text longer than its table: such tokens are not stored and not seen."""
     b = Batch((4, 2, 64), [(40, 6), (20, 2)], BF16, fill=0.0)
