@@ -530,7 +530,7 @@ typedef struct card_row_mask {
  * matter here and is kept (a pool that steps and prompts run on too is cleared once before its first use: they take every slot of
  * a page that they read as finite).  Device data that is out of its range reads and writes nothing outside the buffers: tokens whose page
  * is outside the pool or the table are not stored and not seen.
- * The sums of a row are taken in an order that depends on the sizes of the call (n_rows, n_seqs, max_new, max_len) and
+ * The sums of a row are taken in an order that depends on the sizes of the call (n_rows, n_seqs, table_pages, max_new, max_len) and
  * on its sequence, not on what runs beside it: the same call gives the same bits.
  * Errors: CARD_EINVAL, CARD_ERANGE (layer; n_rows * n_q_heads / 16 + 2 * n_seqs * n_kv_heads >= 2^24), CARD_EDEVICE; nothing is enqueued on error. */
 size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch);
