@@ -131,7 +131,7 @@ def test_attend_of_few_rows_under_tree_masks(heads, dtype):
 @pytest.mark.parametrize("heads,new", [((8, 8, 64), (16, 17, 64, 65)), ((4, 2, 64), (8, 9, 63, 64, 65, 128, 129)), ((4, 1, 128), (4, 5, 64, 65, 80)),
                                        ((8, 1, 64), (2, 3, 32, 33))], ids=lambda v: "_".join("%d" % x for x in v))
 def test_attend_at_the_ends_of_its_variants(heads, new, dtype):
-    """As many rows x heads as one kind of workgroup takes, and one token more; behind texts that are cut and some that are not."""
+    """As many rows x heads as one kind of workgroup takes, and one token more, behind texts of several lengths."""
     for n in new:
         lens = [(19, 1), (419, n), (0, n), (3, 0)]
         Call(Batch(heads, lens, dtype, seed=n)).run().check()
