@@ -521,8 +521,9 @@ typedef struct card_row_mask {
  * rounded to bf16) behind what their sequences hold, then out = softmax(q k / sqrt(head_dim)) v for each new row and query head over the
  * tokens of its sequence up to its own, or over what `mask` lets it see.  A row that sees nothing is zero.
  *   q, out  : n_q_heads heads; k, v: n_kv_heads heads, or both NULL where the cache holds the new tokens already.  All of one
- *             type: CARD_BF16, or CARD_F32, whose products keep 32-bit accuracy.  Data and strides in multiples of 16 bytes;
- *             strides of out at least head_dim; out overlaps no other array.  Rows behind row_starts[n_seqs] are not touched.
+ *             type: CARD_BF16, or CARD_F32, whose products keep 32-bit accuracy.  The softmax is in fp32; of its weights
+ *             16 bits go into the product with v (CARD_BF16) or 24 (CARD_F32).  Data and strides in multiples of 16
+ *             bytes; strides of out at least head_dim; out overlaps no other array.  Rows behind row_starts[n_seqs] are not touched.
  *   mask    : NULL = causal
  *   workspace_dev : card_kv_attend_workspace_bytes, 16-byte aligned (NULL where that is 0), no preparation; calls that may run
  *             at the same time do not share one

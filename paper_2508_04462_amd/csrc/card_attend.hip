@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void k_attend_store(AttendArgs a) {
     }
 }
 
-// Two floats as sums of N bf16, a pair in each word: of one part 8 bits of them, of three all 24.
+// Two floats as sums of N bf16, a pair in each word: of one part 8 bits of them, of two 16, of three all 24.
 template <int N>
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t (&p)[N]) {
     typedef __attribute__((ext_vector_type(2))) float float2v;
@@ -272,10 +272,15 @@ __device__ __forceinline__ UnitCuts cuts_of(const AttendArgs& a, const SeqUnit& 
     return c;
 }
 
-// Scores, maxima, sums and output are held in fp32.  With bf16 rows the weights are rounded to bf16, at most 2^-8 of each, as P V takes them: of
-// the precision of the values that they multiply, and of the result.  (a batch against 64 bits, of the root mean square: 2.3e-3; an fp32
-// softmax with its result rounded to bf16 1.7e-3.)  With fp32 rows q and the weights go in as three parts each (split_pair), 24 bits.
-constexpr float kSlack = 8.f;  // (see below; 0, k_attend_many: 507 -> 545 us, three texts of up to 1000 rows x 7 142 -> 167)
+// Scores, maxima, sums and output are held in fp32.  The weights go into P V as the sum of several bf16 parts (split_pair): with bf16 rows two, 16 bits, as
+// the library's own steps and prompts take theirs, so that rounding the output to bf16 is what its error consists of (a batch against 64 bits, of the
+// root mean square: 1.65e-3, an fp32 softmax rounded to bf16 1.65e-3; with one part 2.3e-3); with fp32 rows three, 24 bits, and q as well.  The
+// sum of the weights takes them in 32 bits, or where it is a product with ones in the same parts, 2^-17 from that at most.  The second part
+// costs nothing where the cache's reading binds (48 texts of a row each 94.2 us, with one part 94.1; 16 rows each 117, 115), and where the matrix
+// units do what their third product takes (2000 rows x 4 behind 14000 tokens 649, 516).
+template <typename T>
+constexpr int kWeightParts = sizeof(T) == 4 ? 3 : 2;
+constexpr float kSlack = 8.f;  // (see below; 0, k_attend_many: 649 -> 686 us, three texts of up to 1000 rows x 7 176 -> 199)
 
 // Floats that a cut leaves of a tile: [16][H], [16] maxima, [16] sums.
 template <int H>
@@ -287,12 +292,12 @@ constexpr int kPartFloats = 16 * (H + 2);
 // meet in LDS, the cuts' in memory, where k_attend_join adds them up.
 // The KV heads of a unit are neighbours in the launch and so go to different compute dies: the dies' shares do not depend on how long which
 // sequence is, and the workgroups of one head, which read the same pages, share an L2 (five rows x 8 behind 32700 tokens 37 us, with the units as neighbours
-// 49; k_attend_many, 2000 rows x 4 behind 14000, 507 and 534; 48 texts of a row each 94.7 and 95.6).
+// 49; k_attend_many, 2000 rows x 4 behind 14000, weights in one part, 507 and 534; 48 texts of a row each 94.7 and 95.6).
 // NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 2 us.
 // 8 KV heads of 128: 48 texts of 400-4000 tokens, 444 MB, in 90 us (4.9 TB/s); 32700 tokens, 134 MB, in 27.
 template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few(AttendArgs a) {
-    constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, LD = H + 4, CH = H / 16;
+    constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16;
     __shared__ union __align__(16) {
         Stage<H> stage;
         float red[4][16][LD];
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
                     for (int n = 0; n < NT; ++n) s[j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j][st], qf[n][w][st], s[j][n], 0, 0, 0);
         if (WHOLE || i + 2 < count) refill_k();
         const bool both = there[0] && there[1];
-        uint2v p[2][NT][NP];
+        uint2v p[2][NT][NW];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             if (!WHOLE || !both) {
@@ -427,10 +432,10 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
                     const float x0 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref));
                     const float x1 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref));
                     sum[n] += x0 + x1;  // (of this lane's keys; the four lanes of a column are added up at the end)
-                    uint32_t pair[NP];
-                    split_pair<NP>(x0, x1, pair);
+                    uint32_t pair[NW];
+                    split_pair<NW>(x0, x1, pair);
 #pragma unroll
-                    for (int q = 0; q < NP; ++q) p[j][n][q][e / 2] = pair[q];
+                    for (int q = 0; q < NW; ++q) p[j][n][q][e / 2] = pair[q];
                 }
         }
         if (!WHOLE || !both) {  // slots that are not the sequence's may hold anything: not multiplied, not even by zero
@@ -444,7 +449,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int q = 0; q < NP; ++q)
+            for (int q = 0; q < NW; ++q)
 #pragma unroll
                 for (int t = 0; t < HT; ++t)
 #pragma unroll
@@ -534,14 +539,16 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
 // through LDS: K as it lies, V with the two pages side by side, so that 16 bytes of a lane are its operand of a matrix instruction over 32
 // tokens.  A round's phases depend on each other, and a compute unit holds two workgroups, so the rounds overlap: while the
 // weights of round i are taken (vector units), the matrix units make the scores of round i + 1; the pages of round i + 2 go to LDS, those of
-// i + 3 are on their way to registers.  Three buffers, one barrier per round.  Per round a wavefront issues 544 clocks of matrix instructions
-// and about 430 of softmax, and LDS is busy for 640 clocks of a workgroup; two rounds take 2200.  2000 rows x 4 behind 14000 tokens, 8 KV heads of 128:
-// 492 GFLOP in 500 us, 0.98 PFLOP/s, the matrix units busy 42 % of the time at 2.1 GHz.  64 rows per wavefront, which would halve the LDS reads,
-// leave a compute unit one workgroup and nothing to overlap with: 995 us.
+// i + 3 are on their way to registers.  Three buffers, one barrier per round.  Per round a wavefront issues 52 matrix instructions, 832 clocks, and 138
+// vector instructions, 16 of them exponentials, and LDS is busy for 640 clocks of a workgroup; two rounds take 2750.  2000 rows x 4 behind 14000
+// tokens, 8 KV heads of 128: 492 GFLOP in 642 us of calls back to back, 0.77 PFLOP/s, with the second part of the weights 738 in products, 1.15, of 1.25 that a
+// large bf16 product reaches here; the matrix units are busy 52 % of the time at 2.1 GHz.  64 rows per wavefront, which would halve the LDS reads,
+// leave a compute unit one workgroup and nothing to overlap with (with weights in one part 507 -> 995).
 constexpr int kManyWaves = 4, kManyTiles = 2 * kManyWaves;  // tiles of 16 rows x heads of a workgroup
 template <int H>
 __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
     using T = __bf16;
+    constexpr int NW = kWeightParts<T>;
     constexpr int ST = H / 32, HT = H / 16, UNITS = ST * 64;  // UNITS: 16 bytes each of a page of one head
     constexpr int PER = UNITS * 2 / 256;                      // of K, and of V, of a thread per round
     __shared__ uint4v sk[3][2][UNITS], sv[3][HT * 64];
@@ -711,21 +718,29 @@ __global__ __launch_bounds__(256, 2) void k_attend_many(AttendArgs a) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const float mref = mx[n] == -INFINITY ? 0.f : mx[n];
-            uint4v w;
+            uint4v w[NW];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; e += 2)
-                    w[j * 2 + e / 2] = pack_pair(__builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref)),
-                                                 __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref)));
-            // The products of a tile stay together, in front of the other workgroup's instructions: 2000 rows x 4 behind 14000 tokens 507 us,
-            // without the priority 521, left to the compiler's order 531.
+                for (int e = 0; e < 4; e += 2) {
+                    uint32_t pair[NW];
+                    const float x0 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e], a.scale, -mref));
+                    const float x1 = __builtin_amdgcn_exp2f(fmaf(s[j][n][e + 1], a.scale, -mref));
+                    split_pair<NW>(x0, x1, pair);
+#pragma unroll
+                    for (int q = 0; q < NW; ++q) w[q][j * 2 + e / 2] = pair[q];
+                }
+            // The products of a tile stay together, in front of the other workgroup's instructions: 2000 rows x 4 behind 14000 tokens 649 us,
+            // without the priority 704, left to the compiler's order 690.
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
-            sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w), sum[n], 0, 0, 0);
 #pragma unroll
-            for (int t = 0; t < HT; ++t)
-                o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], __builtin_bit_cast(bf16x8, w), o[n][t], 0, 0, 0);
+            for (int q = 0; q < NW; ++q) {
+                sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, w[q]), sum[n], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < HT; ++t)
+                    o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], __builtin_bit_cast(bf16x8, w[q]), o[n][t], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
