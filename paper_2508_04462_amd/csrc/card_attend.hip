@@ -52,7 +52,8 @@ __device__ __forceinline__ SeqUnit find_unit(const AttendArgs& a, int unit, int 
     }
     // the last 64: all that is to be known of each, in one round trip
     const int s = min(lo + lane, hi - 1), start = seq_start(a, s), end = seq_start(a, s + 1), held = a.ctx[s];
-    const int at = max(__popcll(__ballot(lo + lane < hi && first(start, s) <= unit)) - 1, 0);
+    const int hits = __popcll(__ballot(lo + lane < hi && first(start, s) <= unit));  // (none: row starts that do not begin at 0)
+    const int at = max(hits - 1, 0);
     SeqUnit u;
     u.seq = __builtin_amdgcn_readfirstlane(lo + at);
     u.row0 = __builtin_amdgcn_readlane(start, at);
