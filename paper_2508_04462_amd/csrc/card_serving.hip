@@ -95,21 +95,23 @@ int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
 }
 
 // How the attention of a call is run.  R: most rows x heads of a KV head that one sequence has; all figures in us, 8 KV heads of 128.
-// Tiles of 16 rows x heads of a workgroup.  R <= 16 one: R = 16 of 16 texts of 300-3000 tokens 25.6, with two 32.5.  R <= 256 two, which
-// read the cache half as often: R = 64 of 48 texts of 400-4000 tokens 115, with one 133, with four (which leave a compute unit one workgroup) 123.  Above,
-// k_attend_many: 16 texts, R = 256: 46 against 71 there, R = 512: 79 against 86; one text of 14000 tokens, R = 512: 54 against 58; 48 texts,
-// R = 384: 246 against 224.  fp32: one, whose three parts of a row fill the registers as more rows would (R = 256: 73, with two 101).
-// The new tokens are stored by the same kernel as long as R <= 256 and they have room in LDS, else by one in front: R = 32 of one text 19.4
-// and 21.6, R = 256 44 and 45 (16 texts 46 and 46), R = 512 82 and 76.
-constexpr int kFewRows = 256;
+// Tiles of 16 rows x heads of a workgroup.  R <= 16 one: R = 16 of 16 texts of 300-3000 tokens 25.8, with two 33.0.  R <= 512 two, which
+// read the cache half as often: R = 64 of 48 texts of 400-4000 tokens 117, with one 134.  Above, k_attend_many.  Two tiles and k_attend_many, R = 384, 512, 768: a
+// text of 14000 tokens 55 and 57, 70 and 67, 108 and 87; of 300 tokens 13 and 18, 13 and 22, 13 and 24; 16 texts of 300-3000 71 and 80, 85 and 98, 119 and
+// 137; 48 of 100-1000 86 and 91, 109 and 109, 154 and 138.  fp32: one, whose three parts of a row fill the registers as more rows would (R = 256: 73,
+// with two 101).
+// The new tokens are stored by the same kernel as long as R <= 256 and they have room in LDS, else by one in front: R = 32 of one text 20.3
+// and 23.0, R = 256 40.6 and 42.7, R = 384 of 16 texts 80 and 71, R = 512 of 48 151 and 109.
+constexpr int kFewRows = 512, kFewStore = 256;
 // The pages of a sequence are cut to have this many workgroups, two per compute unit, unless there are three quarters of them
-// without (one token each, 256, 512, 768, 2048 workgroups: a text of 14000 tokens 16.0, 18.1, 18.1, 21.5; 48 texts of 400-4000 94.5, 93.9, 93.7, 99.1; R = 128,
-// 14000 tokens, 256, 512, 768: 30, 25, 30; k_attend_many, 250 tokens behind 14000: 101, 82, 95).  Counted by rows, so that texts of a few rows, which
-// differ in length, are cut more than that: 48 texts in five cuts 93.9, in two (768 workgroups) 99.6.
+// without (one token each, 256, 512, 768, 2048 workgroups: a text of 14000 tokens 16.1, 18.3, 18.3, 21.4; 48 texts of 400-4000 94.3, 94.2, 93.5, 99.6; R = 128,
+// 14000 tokens, 256, 512, 768: 35, 28, 33; k_attend_many, 250 tokens behind 14000: 121, 98, 115).  Counted by rows, so that texts of a few rows, which
+// differ in length, are cut more than that: 48 texts in five cuts 94.2, in two (768 workgroups) 99.6.
 constexpr int kFill = 512;
 // Cuts cost the join, 3 us and a share per workgroup, and gain where a workgroup's pages take longer: not for so many pages.  (uncut and cut; one token each: a
-// text of 500 tokens 7.3 and 8.4, 1000 10.1 and 8.4; 8 texts of 1000 10.2 and 9.8; 30 of 1000 17.3 and 20.2, of 1500 23.0 and 24.4; 100 of 2000 99 and
-// 102; k_attend_many, 100 tokens behind 200 17.0 and 17.0, behind 500 23.6 and 17.2, 500 behind 500 33.3 and 33.8, behind 1500 56 and 42.)
+// text of 500 tokens 7.6 and 8.4, 1000 11.0 and 8.4; 8 texts of 1000 11.1 and 10.1; 30 of 1000 17.6 and 19.4, of 1500 23.5 and 24.3; 100 of 2000 99 and
+// 100; R = 512 behind 700 tokens 16.5 and 18.2, behind 2000 28.0 and 23.6; k_attend_many, R = 640 behind 100 17.9 and 18.9, behind 700 34 and 24, R = 2000 behind 300 33 and
+// 33, behind 500 39 and 35, behind 1500 67 and 46, R = 4000 behind 1000 69 and 71.)
 int64_t pages_uncut(int tiles, int64_t groups) { return tiles == kManyTiles ? 8 + groups / 2 : 32 + groups / 3; }
 struct AttendPlan {
     int32_t tiles, units, cuts, cut_pages;
@@ -120,7 +122,7 @@ AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
     const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
-    p.fused = most <= std::min(kFewRows, kStage * G);
+    p.fused = most <= std::min(kFewStore, kStage * G);
     p.tiles = f32 || most <= 16 ? 1 : (most <= kFewRows ? 2 : kManyTiles);
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
