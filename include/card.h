@@ -37,7 +37,8 @@ typedef enum card_status {
     CARD_ERANGE = -2,    /* r outside [1, max_r], level / index outside the cache         */
     CARD_ECAPACITY = -3, /* ctx_len + r exceeds max_ctx or the block table                 */
     CARD_EDEVICE = -4,   /* a HIP call failed (launch error, wrong device architecture)    */
-    CARD_ESTALE = -5,    /* cache write refers to an epoch that a correction has ended     */
+    CARD_ESTALE = -5,    /* cache write refers to an epoch that a correction has ended (the Python
+                            package: an attention plan to pages that its sequences gave up) */
     CARD_ETOOBIG = -6    /* card_verify_static: the model's workspace exceeds the scratch   */
 } card_status;
 

@@ -695,7 +695,7 @@ const char* card_strerror(int status) {
         case CARD_ERANGE: return "value out of range";
         case CARD_ECAPACITY: return "KV cache capacity exceeded";
         case CARD_EDEVICE: return "device error";
-        case CARD_ESTALE: return "stale cache epoch";
+        case CARD_ESTALE: return "stale: what the call refers to has changed";
         case CARD_ETOOBIG: return "workspace of this model exceeds the static scratch buffer";
         default: return "unknown status";
     }

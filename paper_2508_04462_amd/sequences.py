@@ -18,11 +18,14 @@ class _Sequence:
 
 class AttendPlan:
     """What the attention calls of one batch share, layer after layer: lengths, row starts and block tables on the device, and a
-    workspace.  Made by SequencePool.plan; the sequences must keep their pages and lengths until its last call has been enqueued."""
+    workspace.  Made by SequencePool.plan; it holds as long as its sequences keep its tokens on its pages, and for calls that store, its rows' pages
+    to themselves.  Calls of one plan run one after the other."""
 
     def __init__(self, pool: "SequencePool", seqs: Sequence[int], new: Sequence[int]):
         dev = pool.device
         held = [pool._seqs[s] for s in seqs]
+        self._pool, self._changes = pool, None
+        self._rows = [(s, list(h.pages), h.length - n, h.length) for s, h, n in zip(seqs, held, new)]
         width = max(1, max(len(h.pages) for h in held))
         starts = [0]
         for n in new:
@@ -35,6 +38,15 @@ class AttendPlan:
         self.batch = B.CardKVBatch(pool.k_pages.data_ptr(), pool.v_pages.data_ptr(), pool.n_pages, self.n_seqs, self.tables.data_ptr(), width,
                                    self.n_rows, self.ctx_lens.data_ptr(), self.row_starts.data_ptr(), max(new), max(h.length for h in held))
         self.workspace = torch.empty(B.card_kv_attend_workspace_bytes(pool.cfg, self.batch), dtype=torch.uint8, device=dev)
+
+    def _look_again(self) -> None:
+        """What the pool's changes since the last look leave of the plan."""
+        pool = self._pool
+        if self._changes == pool._changes:
+            return
+        self._changes = pool._changes
+        self._reads = all(s in pool._seqs and pool._seqs[s].length >= end and pool._seqs[s].pages[:len(pages)] == pages for s, pages, _, end in self._rows)
+        self._stores = self._reads and all(pool.writable(s, first, end) for s, _, first, end in self._rows)
 
 
 class SequencePool:
@@ -61,6 +73,7 @@ class SequencePool:
         self._users = [0] * self.n_pages
         self._seqs: Dict[int, _Sequence] = {}
         self._next = 0
+        self._changes = 0  # of what sequences hold and share
 
     # -- bookkeeping
     @property
@@ -77,6 +90,7 @@ class SequencePool:
         return seq
 
     def free(self, seq: int) -> None:
+        self._changes += 1
         for p in self._seqs.pop(seq).pages:
             self._release(p)
 
@@ -85,6 +99,7 @@ class SequencePool:
         s = self._seqs[seq]
         if not 0 <= length <= s.length:
             raise B.CardError(B.CARD_ERANGE, "truncate")
+        self._changes += 1
         keep = (length + 15) // 16
         for p in s.pages[keep:]:
             self._release(p)
@@ -96,6 +111,7 @@ class SequencePool:
         s = self._seqs[seq]
         if n < 0:
             raise B.CardError(B.CARD_ERANGE, "extend")
+        self._changes += 1
         if s.length + n > self.cfg.max_ctx:
             raise B.CardError(B.CARD_ECAPACITY, "extend")
         need = (s.length + n + 15) // 16 - len(s.pages)
@@ -109,11 +125,13 @@ class SequencePool:
         s.length += n
 
     def fork(self, seq: int) -> int:
-        """A sequence of the same tokens: full pages are shared, the last one, which both may go on writing, is copied."""
+        """A sequence of the same tokens: full pages are shared, the last one, which both may go on writing, is copied as the calls before have
+        left it."""
         s = self._seqs[seq]
         tail = s.length % 16 != 0
         if tail and not self._free:
             raise B.CardError(B.CARD_ECAPACITY, "fork")
+        self._changes += 1
         other = self.new()
         t = self._seqs[other]
         t.length, t.pages = s.length, list(s.pages)
@@ -165,7 +183,8 @@ class SequencePool:
     def attend(self, plan: AttendPlan, layer: int, q: torch.Tensor, k: Optional[torch.Tensor], v: Optional[torch.Tensor],
                out: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None, mask_base: Optional[torch.Tensor] = None) -> torch.Tensor:
         """card_kv_attend of the plan's rows: q and out [rows][query heads][h], k and v [rows][kv heads][h] (None: stored before), bf16 or
-        fp32; mask int32 [rows][words] with mask_base int32 [sequences]."""
+        fp32; mask int32 [rows][words] with mask_base int32 [sequences].  CARD_ESTALE, and nothing happens, where the plan does not hold any more: its
+        sequences have given up its tokens or pages, or it is to store to pages that a fork holds since."""
         cfg = self.cfg
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
         for t, heads in ((q, cfg.n_q_heads), (k, cfg.n_kv_heads), (v, cfg.n_kv_heads), (out, cfg.n_q_heads)):
@@ -180,6 +199,9 @@ class SequencePool:
             row_mask = B.CardRowMask(mask.data_ptr(), mask_base.data_ptr(), mask.shape[1])
         if plan.n_rows == 0:
             return out
+        plan._look_again()
+        if not (plan._reads if k is None else plan._stores):
+            raise B.CardError(B.CARD_ESTALE, "attend")
         rows = [None if t is None else B.card_rows(t) for t in (q, k, v, out)]
         stream = torch.cuda.current_stream(self.device)
         if stream != plan.stream:  # the plan may be dropped before that stream has got to the call
@@ -212,6 +234,7 @@ class SequencePool:
         """Copies of these shared pages take their places."""
         if not places:
             return
+        self._changes += 1
         src = [s.pages[i] for i in places]
         dst = [self._take() for _ in places]
         kv = B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), None, self.n_pages, -1)
