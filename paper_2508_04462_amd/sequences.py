@@ -199,6 +199,8 @@ class SequencePool:
             row_mask = B.CardRowMask(mask.data_ptr(), mask_base.data_ptr(), mask.shape[1])
         if plan.n_rows == 0:
             return out
+        if plan._pool is not self:
+            raise ValueError("a plan of another pool")
         plan._look_again()
         if not (plan._reads if k is None else plan._stores):
             raise B.CardError(B.CARD_ESTALE, "attend")

@@ -116,6 +116,19 @@ def test_a_shared_page_that_gets_a_copy(pool):
     assert pool.run(late) and pool.run(rows) and plan.n_rows == 0
 
 
+def test_plan_of_another_pool(pool, monkeypatch):
+    """Its pages are others, whatever its rows look like."""
+    other = AttendingPool(monkeypatch)
+    plans = []
+    for p in (pool, other):
+        a = _sequence(p, 20)
+        plans.append(p.plan([a], [4]))
+    for p, plan in ((pool, plans[1]), (other, plans[0])):
+        with pytest.raises(ValueError):
+            p.run(plan)
+    assert other.run(plans[1]) and other.calls == 1
+
+
 def test_changes_elsewhere_do_not_matter(pool):
     a, b = _sequence(pool, 10), _sequence(pool, 40)
     pool.extend(a, 2)
