@@ -52,7 +52,8 @@ class AttendPlan:
 class SequencePool:
     """Pages of one model's cache, shared by sequences that come and go.  A sequence has a length and the pages for it; a fork shares
     the pages that are full and copies the last one.  Pages that several sequences hold are never written: what would write to one
-    gets a copy first.  Pools start cleared.  One thread at a time; device work goes to the current stream, in the order of the calls.
+    gets a copy first.  A new page's values are zero, whoever held it before: steps and prompts multiply the places behind a text's end with weights of
+    zero.  One thread at a time; device work goes to the current stream, in the order of the calls.
 
     Steps and prompts of a Target run on a sequence after Target.attach; a program with its own layers stores and attends
     through attend()."""
@@ -71,6 +72,7 @@ class SequencePool:
         self.v_pages = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         self._free = list(range(self.n_pages - 1, -1, -1))
         self._users = [0] * self.n_pages
+        self._written = [False] * self.n_pages  # pages that some sequence has held
         self._seqs: Dict[int, _Sequence] = {}
         self._next = 0
         self._changes = 0  # of what sequences hold and share
@@ -120,8 +122,12 @@ class SequencePool:
             raise B.CardError(B.CARD_ECAPACITY, "extend")
         self._own(s, shared)
         if need > 0:
+            again = any(self._written[p] for p in self._free[-need:])
             s.pages += [self._take() for _ in range(need)]
             self._upload(s)
+            if again:
+                values = self.v_pages.view(torch.int64).view(self.cfg.n_layers, self.n_pages, -1)
+                values.index_fill_(1, s.table[len(s.pages) - need:len(s.pages)].long(), 0)
         s.length += n
 
     def fork(self, seq: int) -> int:
@@ -218,7 +224,7 @@ class SequencePool:
 
     def _take(self) -> int:
         p = self._free.pop()
-        self._users[p] = 1
+        self._users[p], self._written[p] = 1, True
         return p
 
     def _release(self, p: int) -> None:

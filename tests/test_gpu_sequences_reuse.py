@@ -1,0 +1,42 @@
+"""Pages of a SequencePool that pass from one text to another."""
+import pytest
+import torch
+
+from test_gpu_sequences import SHAPE, _step, _tokens, target  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _store(pool, seq, n, seed, values=None):
+    """The next n tokens of a sequence, in all layers, through attend()."""
+    pool.extend(seq, n)
+    plan = pool.plan([seq], [n])
+    g = torch.Generator().manual_seed(seed)
+    for layer in range(SHAPE.n_layers):
+        q, k, v = (torch.randn((n, heads, SHAPE.head_dim), generator=g).bfloat16().cuda() for heads in (8, 2, 2))
+        pool.attend(plan, layer, q, k, v if values is None else torch.full_like(v, values))
+
+
+def test_a_step_behind_tokens_on_another_texts_pages(target):  # noqa: F811
+    """The text before left NaN and infinities; a step in the middle of a page that attend() opened is what it is on a new pool."""
+    import paper_2508_04462_amd as card
+
+    got = []
+    try:
+        for before in (None, float("nan"), float("inf")):
+            pool = card.SequencePool(SHAPE, 6, 512)
+            if before is not None:
+                a = pool.new()
+                _store(pool, a, 90, 1, before)
+                pool.free(a)
+            b = pool.new()
+            _store(pool, b, 20, 2)
+            target.attach(pool, b)
+            pool.extend(b, 4)
+            got.append(_step(target, 20, _tokens(40, 4)))
+            pool.extend(b, 30)
+            got.append(_step(target, 24, _tokens(41, 8)))
+    finally:
+        target.attach()
+    assert all(torch.isfinite(x).all() for x in got)
+    assert torch.equal(got[2], got[0]) and torch.equal(got[4], got[0]) and torch.equal(got[3], got[1]) and torch.equal(got[5], got[1])

@@ -184,3 +184,27 @@ def test_plans_against_what_sequences_hold(pool):
             assert pool.run(plan) == own and pool.run(plan, store=False) == there
             taken, refused = taken + own, refused + (not own)
     assert taken > 500 and refused > 500
+
+
+def test_pages_of_an_ended_text_are_cleared_for_the_next(monkeypatch):
+    """Steps multiply the values behind a text's end with weights of zero: what its last owner left there, NaN perhaps, must not be in a page that is
+    taken from the free ones.  Pages that a sequence holds, copies among them, keep what they have."""
+    pool = PlayedPool(monkeypatch, 12, 160)
+    values = pool.v_pages.view(torch.bfloat16).view(pool.cfg.n_layers, 12, -1)
+    a, b = _sequence(pool, 40), _sequence(pool, 20)
+    old = list(pool._seqs[a].pages)
+    values[:, old + pool._seqs[b].pages] = float("nan")
+    kept = list(pool._seqs[b].pages)
+    pool.free(a)
+    c = _sequence(pool, 10)
+    pool.extend(c, 100)
+    mine = pool._seqs[c].pages
+    assert set(old) <= set(mine) and (values[:, mine] == 0).all()
+    assert values[:, kept].isnan().all()
+    # truncated pages, too; a copy of a shared page is a copy
+    values[:, mine] = 1.0
+    pool.truncate(c, 50)
+    d = pool.fork(c)
+    assert pool._seqs[d].pages[:3] == mine[:3]
+    pool.extend(b, 30)
+    assert (values[:, pool._seqs[b].pages[2:]] == 0).all() and values[:, kept].isnan().all() and (values[:, mine[:4]] == 1.0).all()
