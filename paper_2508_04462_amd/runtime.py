@@ -148,7 +148,7 @@ class Target:
         max_ctx, the positions that they write being among those that it has been extended to; without arguments, on the Target's own pages again."""
         if pool is not None:
             a, b = self.cfg, pool.cfg
-            if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.device:
+            if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.k_pages.device:
                 raise ValueError("a pool of other layers or heads, or on another device")
             if b.max_ctx < a.max_ctx:  # calls may look at as many places of the block table
                 raise ValueError("a pool of shorter sequences")

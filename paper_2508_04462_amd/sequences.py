@@ -64,12 +64,13 @@ class SequencePool:
         self._setup(make_cfg(shape, max_ctx), n_pages, torch.device(device))
 
     def _setup(self, cfg, n_pages: int, device) -> None:
-        self.cfg, self.device, self.n_pages = cfg, device, int(n_pages)
+        self.cfg, self.n_pages = cfg, int(n_pages)
         nbytes = B.card_kv_pool_bytes(self.cfg, self.n_pages)
         if nbytes == 0:
             raise B.CardError(B.CARD_EINVAL, "card_kv_pool_bytes")
         self.k_pages = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         self.v_pages = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.device = self.k_pages.device  # ("cuda" has become the device that was current)
         self._free = list(range(self.n_pages - 1, -1, -1))
         self._users = [0] * self.n_pages
         self._written = [False] * self.n_pages  # pages that some sequence has held

@@ -40,3 +40,26 @@ def test_a_step_behind_tokens_on_another_texts_pages(target):  # noqa: F811
         target.attach()
     assert all(torch.isfinite(x).all() for x in got)
     assert torch.equal(got[2], got[0]) and torch.equal(got[4], got[0]) and torch.equal(got[3], got[1]) and torch.equal(got[5], got[1])
+
+
+def test_pool_and_target_on_the_current_device(target):  # noqa: F811
+    """"cuda" is the device that is current when pool or Target are made: the same memory, whatever it is called."""
+    import paper_2508_04462_amd as card
+
+    pool = card.SequencePool(SHAPE, 6, 512, device="cuda")
+    assert pool.device == torch.device("cuda", torch.cuda.current_device())
+    a = pool.new()
+    pool.extend(a, 20)
+    other = card.Target(SHAPE, 512, device="cuda")
+    other.packed = target.packed
+    try:
+        target.attach(pool, a)
+        token = target.prefill(_tokens(42, 20))
+        pool.truncate(a, 0)
+        pool.extend(a, 20)
+        other.attach(pool, a)
+        assert other.prefill(_tokens(42, 20)) == token
+        here = card.SequencePool(SHAPE, 6, 512)
+        other.attach(here, here.new())
+    finally:
+        target.attach()
