@@ -167,7 +167,8 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, const LogprobSh
     const T* x = static_cast<const T*>(a.logits) + int64_t(row) * a.row_stride;
     const float ln_s = logf(r.s);
     const bool is_void = r.s != r.s, empty = r.s == 0.f;
-    const auto logprob = [&](float v) { return is_void ? NAN : (empty ? -INFINITY : (v - r.m) * a.inv_temp - ln_s); };
+    // (of halves: the difference of two logits may be beyond the largest float where the quotient is not)
+    const auto logprob = [&](float v) { return is_void ? NAN : (empty ? -INFINITY : (0.5f * v - 0.5f * r.m) * a.inv_temp * 2.f - ln_s); };
     if (tid < a.top) {
         const unsigned long long key = sm.out[tid];
         const bool none = is_void || key == 0ull;
