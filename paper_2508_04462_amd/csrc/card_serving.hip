@@ -23,7 +23,7 @@ inline size_t layer_elems(const card_model_cfg* cfg, int32_t n_pages) { return s
 class NumberSet {
 public:
     explicit NumberSet(int32_t n) {
-        while (size_ < 2 * size_t(n)) size_ *= 2;
+        for (; size_ < 2 * size_t(n); size_ *= 2) --shift_;
         at_ = static_cast<int32_t*>(malloc(size_ * sizeof(int32_t)));
         if (at_) std::fill(at_, at_ + size_, -1);
     }
@@ -41,11 +41,12 @@ public:
 
 private:
     size_t place(int32_t v) const {
-        size_t i = (uint32_t(v) * 0x9e3779b1u) & (size_ - 1);
+        size_t i = (uint32_t(v) * 0x9e3779b1u) >> shift_;  // the upper bits: numbers that lie a power of two apart spread, too
         while (at_[i] != -1 && at_[i] != v) i = (i + 1) & (size_ - 1);
         return i;
     }
     size_t size_ = 16;
+    int shift_ = 28;  // 32 - log2(size_)
     int32_t* at_ = nullptr;
 };
 
