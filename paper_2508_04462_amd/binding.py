@@ -371,6 +371,7 @@ def card_kv_gather(cfg, kv: CardKV, layer: int, first_slot: int, count: int, k_o
 
 
 def card_kv_copy_pages(cfg, kv: CardKV, src_pages, dst_pages, stream=None) -> int:
+    """Lists of numbers, or ctypes arrays of int32, which the library reads as they are (so does card_kv_move_slots)."""
     if len(src_pages) != len(dst_pages):
         return CARD_EINVAL
     return lib.card_kv_copy_pages(cfg, kv, len(src_pages), _i32(src_pages), _i32(dst_pages), _ptr(stream))

@@ -295,7 +295,7 @@ constexpr int kPartFloats = 16 * (H + 2);
 // sequence is, and the workgroups of one head, which read the same pages, share an L2 (five rows x 8 behind 32700 tokens 37 us, with the units as neighbours
 // 49; k_attend_many, 2000 rows x 4 behind 14000, weights in one part, 507 and 534; 48 texts of a row each 94.7 and 95.6).
 // NEW: the call's keys and values are taken from its arrays and stored on the way; a kernel in front that stores them costs 2 us.
-// 8 KV heads of 128: 48 texts of 400-4000 tokens, 444 MB, in 90 us (4.9 TB/s); 32700 tokens, 134 MB, in 27.
+// 8 KV heads of 128: 48 texts of 400-4000 tokens, 444 MB, in 90 us (4.9 TB/s); 32700 tokens, 134 MB, in 28.
 template <int H, typename T, int NT, bool NEW>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16;
@@ -542,8 +542,8 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend_few
 // weights of round i are taken (vector units), the matrix units make the scores of round i + 1; the pages of round i + 2 go to LDS, those of
 // i + 3 are on their way to registers.  Three buffers, one barrier per round.  Per round a wavefront issues 52 matrix instructions, 832 clocks, and 138
 // vector instructions, 16 of them exponentials, and LDS is busy for 640 clocks of a workgroup; two rounds take 2750.  2000 rows x 4 behind 14000
-// tokens, 8 KV heads of 128: 492 GFLOP in 642 us of calls back to back, 0.77 PFLOP/s, with the second part of the weights 738 in products, 1.15, of 1.25 that a
-// large bf16 product reaches here; the matrix units are busy 52 % of the time at 2.1 GHz.  64 rows per wavefront, which would halve the LDS reads,
+// tokens, 8 KV heads of 128: 492 GFLOP in 655 us, 0.75 PFLOP/s, with the second part of the weights 738 GFLOP of products, 1.13, where a large bf16
+// product reaches 1.25 here; the matrix units are busy 52 % of the time at 2.1 GHz.  64 rows per wavefront, which would halve the LDS reads,
 // leave a compute unit one workgroup and nothing to overlap with (with weights in one part 507 -> 995).
 constexpr int kManyWaves = 4, kManyTiles = 2 * kManyWaves;  // tiles of 16 rows x heads of a workgroup
 template <int H>

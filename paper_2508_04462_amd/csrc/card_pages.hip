@@ -37,7 +37,7 @@ struct MoveArgs {
 // wrote, and so is reading the next ROUND while these are written.  No barrier, and two rounds under way.  The host puts gaps into the list so that
 // slots that go to four neighbours in a row begin at a multiple of four.
 // 1500 tokens of 32 layers x 8 heads x 128, closing gaps of 600 between them, us: a move at a time, a thread per element, 720; rounds of 96
-// moves 124 (471 MB with the gaps' share of the lines: 3.8 TB/s).
+// moves 125 in the kernels (471 MB with the gaps' share of the lines: 3.8 TB/s), 138 a call of four launches.
 // Rounds of 32 for short lists, which are a matter of latency: 128 moves in rounds of 32 and of 96 12.6 and 14.6, 192 17.7 and 20.7, 256 21.8 and
 // 20.8, 1500 136 and 124 (of 64, 128 moves: 1500 128, 129; 128 14.8, 18.8); 16 layers, 192 12.4 and 14.6, 256 15.6 and 14.1, 1500 91 and 74.
 constexpr int kMoveRound = 96, kMoveShort = 32;

@@ -145,7 +145,8 @@ class Target:
 
     def attach(self, pool=None, seq: int = 0) -> None:
         """Steps, prompts and drafts from here on run on sequence `seq` of a SequencePool of the same layers and heads and at least the Target's
-        max_ctx, the positions that they write being among those that it has been extended to; without arguments, on the Target's own pages again."""
+        max_ctx, the positions that they write being among those that it has been extended to (nothing extends it on the way: before a loop
+        over many steps, by all that they write); without arguments, on the Target's own pages again."""
         if pool is not None:
             a, b = self.cfg, pool.cfg
             if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.k_pages.device:

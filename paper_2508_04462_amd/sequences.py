@@ -179,7 +179,8 @@ class SequencePool:
         return B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self._seqs[seq].table.data_ptr(), self.n_pages, int(pending))
 
     def plan(self, seqs: Sequence[int], new: Sequence[int]) -> AttendPlan:
-        """A batch: the last new[i] tokens of sequence seqs[i] (extended by them before) are the rows of the calls."""
+        """A batch: the last new[i] tokens of sequence seqs[i] (extended by them before) are the rows of the calls.  Uploads lengths and tables, and so waits
+        for the current stream, as extend, fork and compact do where a sequence's pages change."""
         if not seqs or len(seqs) != len(new) or len(set(seqs)) != len(seqs):
             raise ValueError("as many numbers of new tokens as sequences, at least one, each sequence once")
         for s, n in zip(seqs, new):
