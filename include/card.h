@@ -540,6 +540,51 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
                    const card_rows* k, const card_rows* v, const card_rows* out, const card_row_mask* mask,
                    void* workspace_dev, void* stream);
 
+/* Rotary embedding of new tokens on their way to the cache, and the storing of their keys and values, one layer: with angles t_j = position * f_j, elements
+ * j and j + head_dim / 2 of each head of q and k become x_j cos t_j - x_(j + h/2) sin t_j and x_(j + h/2) cos t_j + x_j sin t_j; k and v go to
+ * the pages (rounded to bf16) behind what their sequences hold.  card_kv_attend without k and v then attends.
+ *   rotation : NULL: keys are stored as they are (q and q_out then are NULL, too)
+ *   q, q_out : n_q_heads heads, or both NULL where queries are not rotated; q_out may be q, or overlaps no array of the call.  Strides of
+ *              q_out at least head_dim
+ *   k, v     : n_kv_heads heads; they are not changed.  All of one type, CARD_BF16 or CARD_F32, data and strides in multiples of 16 bytes
+ * Angles are made in 64 bits and products added in 64: what is stored or put out is the exact value rounded to its type, from
+ * cosines and sines rounded to fp32.  Rows behind row_starts[n_seqs] are not touched; tokens whose page is outside the pool or the table are not stored,
+ * their queries are rotated all the same.  Only the slots of new tokens are written (a pool that steps and prompts run on too: card_kv_attend).
+ * Errors: CARD_EINVAL (also for frequencies that are not finite), CARD_ERANGE (as card_kv_attend), CARD_EDEVICE; nothing is enqueued on error. */
+typedef struct card_rotation {
+    const double* freqs_host;     /* head_dim / 2 frequencies, radians a position, host memory that is read during the call only; NULL: rope_theta^(-2 j / head_dim) */
+    const int32_t* positions_dev; /* dev [n_rows], e.g. of a tree's nodes; NULL: the places in their sequences */
+} card_rotation;
+int card_kv_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
+                   const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The same cache in 4 bits a value: 3.5 times as many tokens in the same memory (head_dim * 9 / 16 bytes of K and as many of V for a token of a
+ * head, a layer), and as much less to read.  Each 64 channels of a token have a scale and an offset of their own: with the group's lowest and highest
+ * values low and high, m the larger of their magnitudes,
+ *   scale = bf16((high - low) 17 / 256 + m / 1024), and of the fp32 numbers whose lower 16 bits are the scale's the one whose bits are nearest to
+ *   those of low - m / 128 - 16 scale is the offset;
+ *   code = (x - offset) / scale - 16, rounded, in 0 .. 15, and stands for scale * (16 + code) + offset:
+ * at most half a scale (and 2^-16 of one) from x, for magnitudes of 2^-100 to 2^100 or 0; a group with a value that is not finite stands for NaN.  card_kv_batch and card_kv are as above, but for
+ * pools of card_kv4_pool_bytes(cfg, n_pages) bytes each, 16-byte aligned: page p of layer l and KV head a begins at byte
+ * ((l * n_pages + p) * n_kv_heads + a) * 9 * head_dim.  Steps, prompts, drafts and the functions above take pools of 16 bits only, those
+ * here pools of 4 only.  The pools need no initialisation.
+ *
+ * card_kv4_append  : card_kv_append; rotated keys go to their codes unrounded.
+ * card_kv4_read    : what the cache holds of the rows of a batch: k and v [rows][n_kv_heads], strides at least head_dim.  Rows of tokens
+ *                    without a page are not touched.
+ * card_kv4_attend  : card_kv_attend over the values that the codes stand for.  Codes enter the products exactly; what a row does not see may hold anything, also
+ *                    NaN.  The other sentences on card_kv_attend hold here.
+ * card_kv4_copy_pages, card_kv4_move_slots: as card_kv_copy_pages and card_kv_move_slots; codes, scales and offsets move as they are.
+ * ---------------------------------------------------------------------------------------- */
+size_t card_kv4_pool_bytes(const card_model_cfg* cfg, int32_t n_pages);
+int card_kv4_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
+                    const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream);
+int card_kv4_read(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* k, const card_rows* v, void* stream);
+size_t card_kv4_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch);
+int card_kv4_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
+                    const card_rows* v, const card_rows* out, const card_row_mask* mask, void* workspace_dev, void* stream);
+
 /* Log probabilities of given tokens, with the entropy and the most probable tokens of their distributions, p = softmax(logits / temperature).
  *   logits_dev : [rows][vocab], CARD_F32 or CARD_BF16, row_stride elements apart (>= vocab)
  *   tokens_dev : int32 [rows], or NULL; logprob_dev: fp32 [rows] (with tokens_dev): ln p of the token; 0 where the token is

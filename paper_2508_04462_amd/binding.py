@@ -74,6 +74,10 @@ class CardRowMask(C.Structure):
     _fields_ = [("mask_dev", C.c_void_p), ("mask_base_dev", C.c_void_p), ("words", C.c_int32)]
 
 
+class CardRotation(C.Structure):
+    _fields_ = [("freqs_host", C.c_void_p), ("positions_dev", C.c_void_p)]
+
+
 class CardSampling(C.Structure):
     _fields_ = [("temperature", C.c_float), ("seed", C.c_uint64)]
 
@@ -173,6 +177,17 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.card_kv_attend_workspace_bytes.argtypes = [_cfgp, C.POINTER(CardKVBatch)]
     lib.card_kv_attend.restype = C.c_int
     lib.card_kv_attend.argtypes = [_cfgp, C.POINTER(CardKVBatch), C.c_int32, _rowsp, _rowsp, _rowsp, _rowsp, C.POINTER(CardRowMask), _P, _P]
+    for _n in ("card_kv_append", "card_kv4_append"):
+        getattr(lib, _n).restype = C.c_int
+        getattr(lib, _n).argtypes = [_cfgp, C.POINTER(CardKVBatch), C.c_int32, C.POINTER(CardRotation), _rowsp, _rowsp, _rowsp, _rowsp, _P]
+    lib.card_kv4_pool_bytes.restype = C.c_size_t
+    lib.card_kv4_pool_bytes.argtypes = [_cfgp, C.c_int32]
+    lib.card_kv4_read.restype = C.c_int
+    lib.card_kv4_read.argtypes = [_cfgp, C.POINTER(CardKVBatch), C.c_int32, _rowsp, _rowsp, _P]
+    lib.card_kv4_attend_workspace_bytes.restype = C.c_size_t
+    lib.card_kv4_attend_workspace_bytes.argtypes = [_cfgp, C.POINTER(CardKVBatch)]
+    lib.card_kv4_attend.restype = C.c_int
+    lib.card_kv4_attend.argtypes = lib.card_kv_attend.argtypes
     lib.card_logprobs_workspace_bytes.restype = C.c_size_t
     lib.card_logprobs_workspace_bytes.argtypes = [C.c_int32] * 3
     lib.card_logprobs.restype = C.c_int
@@ -410,6 +425,51 @@ def card_kv_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:
 def card_kv_attend(cfg, batch: CardKVBatch, layer: int, q: CardRows, k: Optional[CardRows], v: Optional[CardRows], out: CardRows,
                    mask: Optional[CardRowMask], workspace_dev, stream=None) -> int:
     return lib.card_kv_attend(cfg, batch, layer, q, k, v, out, mask, _ptr(workspace_dev), _ptr(stream))
+
+
+def card_rotation(freqs=None, positions=None) -> CardRotation:
+    """freqs: head_dim / 2 frequencies (None: the model's); positions: int32 [rows] on the device, contiguous (None: the places in the sequences).  It
+    keeps the frequencies; the positions are the caller's to keep."""
+    table = None if freqs is None else (C.c_double * len(freqs))(*[float(f) for f in freqs])
+    rotation = CardRotation(None if table is None else C.addressof(table), _ptr(positions))
+    rotation.table = table
+    return rotation
+
+
+def card_kv_append(cfg, batch: CardKVBatch, layer: int, rotation: Optional[CardRotation], q: Optional[CardRows], q_out: Optional[CardRows],
+                   k: CardRows, v: CardRows, stream=None) -> int:
+    if rotation is not None and _freqs_missing(cfg, rotation):
+        return CARD_EINVAL
+    return lib.card_kv_append(cfg, batch, layer, rotation, q, q_out, k, v, _ptr(stream))
+
+
+def _freqs_missing(cfg, rotation: CardRotation) -> bool:
+    table = getattr(rotation, "table", None)
+    return table is not None and 2 * len(table) != cfg.head_dim
+
+
+def card_kv4_pool_bytes(cfg, n_pages: int) -> int:
+    return lib.card_kv4_pool_bytes(cfg, n_pages)
+
+
+def card_kv4_append(cfg, batch: CardKVBatch, layer: int, rotation: Optional[CardRotation], q: Optional[CardRows], q_out: Optional[CardRows],
+                    k: CardRows, v: CardRows, stream=None) -> int:
+    if rotation is not None and _freqs_missing(cfg, rotation):
+        return CARD_EINVAL
+    return lib.card_kv4_append(cfg, batch, layer, rotation, q, q_out, k, v, _ptr(stream))
+
+
+def card_kv4_read(cfg, batch: CardKVBatch, layer: int, k: CardRows, v: CardRows, stream=None) -> int:
+    return lib.card_kv4_read(cfg, batch, layer, k, v, _ptr(stream))
+
+
+def card_kv4_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:
+    return lib.card_kv4_attend_workspace_bytes(cfg, batch)
+
+
+def card_kv4_attend(cfg, batch: CardKVBatch, layer: int, q: CardRows, k: Optional[CardRows], v: Optional[CardRows], out: CardRows,
+                    mask: Optional[CardRowMask], workspace_dev, stream=None) -> int:
+    return lib.card_kv4_attend(cfg, batch, layer, q, k, v, out, mask, _ptr(workspace_dev), _ptr(stream))
 
 
 def card_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:

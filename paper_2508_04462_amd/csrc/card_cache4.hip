@@ -1,0 +1,133 @@
+// C ABI of rotation with storing, and of the cache of 4 bits a value: argument checks and launches.
+#include <algorithm>
+#include <cmath>
+#include <hip/hip_runtime.h>
+
+#include "card.h"
+#include "card_append.hip"
+#include "card_attend4.hip"
+#include "card_serving.h"
+
+using namespace card;
+
+namespace {
+
+// How the attention of a call is run: as over a cache of 16 bits.
+constexpr int kFewRows4 = 512;
+constexpr int kFill = 512;
+int64_t pages_uncut(int64_t groups) { return 32 + groups / 3; }
+AttendPlan attend4_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f32) {
+    AttendPlan p = {};
+    const int G = cfg->n_q_heads / cfg->n_kv_heads;
+    const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
+    p.tiles = f32 || most <= 16 ? 1 : 2;
+    p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
+    const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
+    const int full = p.units - b->n_seqs + 1;  // tiles, if the rows filled them
+    const int64_t groups = int64_t(full) * cfg->n_kv_heads;
+    const bool whole = groups * 4 > kFill * 3 || pages <= pages_uncut(int64_t(std::max(full, b->n_seqs)) * cfg->n_kv_heads);
+    p.cut_pages = whole ? pages : std::max(16, ceil_div(ceil_div(groups * pages, kFill), 16) * 16);
+    p.cuts = ceil_div(pages, p.cut_pages);
+    if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
+    return p;
+}
+template <int H, typename T>
+void append_launch(const AppendArgs& g, int bits, hipStream_t st) {
+    const dim3 grid(uint32_t(g.a.n_rows / 16 + kStoreUnits * g.a.n_seqs), uint32_t(g.a.Hkv));
+    if (bits == 16) hipLaunchKernelGGL((k_append<H, T, 16>), grid, dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((k_append<H, T, 4>), grid, dim3(256), 0, st, g);
+}
+template <typename T>
+void append_launch(const AppendArgs& g, int bits, int h, hipStream_t st) {
+    h == 128 ? append_launch<128, T>(g, bits, st) : append_launch<64, T>(g, bits, st);
+}
+template <int H, typename T, int NT>
+void attend4_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+    const dim3 grid(uint32_t(p.units) * uint32_t(a.Hkv), uint32_t(p.cuts));
+    hipLaunchKernelGGL((k_attend4_few<H, T, NT>), grid, dim3(256), 0, st, a);
+    if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, 4 * NT), dim3(256), 0, st, a);
+}
+template <typename T, int NT>
+void attend4_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t st) {
+    h == 128 ? attend4_launch<128, T, NT>(a, p, st) : attend4_launch<64, T, NT>(a, p, st);
+}
+
+int append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, int bits, const card_rotation* rotation, const card_rows* q,
+           const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream) {
+    if (const int st = layer_refused(cfg, batch, layer)) return st;
+    if (batch->n_rows == 0) return CARD_OK;
+    if (!k || !v || (k->type != CARD_BF16 && k->type != CARD_F32) || !rows_ok(k, k->type, 0) || !rows_ok(v, k->type, 0)) return CARD_EINVAL;
+    if (!q != !q_out || (q && !rotation)) return CARD_EINVAL;
+    if (q && (!rows_ok(q, k->type, 0) || !rows_ok(q_out, k->type, cfg->head_dim))) return CARD_EINVAL;
+    const int h = cfg->head_dim;
+    AppendArgs g = {};
+    g.a = attend_args(cfg, batch, layer, bits, q, k, v, q_out, nullptr, AttendPlan{}, nullptr);
+    if (rotation) {
+        g.rotate = 1;
+        g.positions = rotation->positions_dev;
+        for (int j = 0; j < h / 2; ++j) {
+            const double f = rotation->freqs_host ? rotation->freqs_host[j] : std::pow(double(cfg->rope_theta), -2.0 * j / h);
+            if (!std::isfinite(f)) return CARD_EINVAL;
+            g.turns[j] = f / 6.283185307179586476925;
+        }
+    }
+    k->type == CARD_F32 ? append_launch<float>(g, bits, h, as_stream(stream)) : append_launch<__bf16>(g, bits, h, as_stream(stream));
+    return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int card_kv_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
+                   const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream) {
+    return append(cfg, batch, layer, 16, rotation, q, q_out, k, v, stream);
+}
+
+size_t card_kv4_pool_bytes(const card_model_cfg* cfg, int32_t n_pages) {
+    return cfg_valid(cfg) && n_pages > 0 ? size_t(cfg->n_layers) * layer4_bytes(cfg, n_pages) : 0;
+}
+
+int card_kv4_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
+                    const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream) {
+    return append(cfg, batch, layer, 4, rotation, q, q_out, k, v, stream);
+}
+
+int card_kv4_read(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* k, const card_rows* v, void* stream) {
+    if (const int st = layer_refused(cfg, batch, layer)) return st;
+    if (batch->n_rows == 0) return CARD_OK;
+    const int h = cfg->head_dim;
+    if (!k || !v || (k->type != CARD_BF16 && k->type != CARD_F32) || !rows_ok(k, k->type, h) || !rows_ok(v, k->type, h)) return CARD_EINVAL;
+    const AttendArgs a = attend_args(cfg, batch, layer, 4, nullptr, k, v, nullptr, nullptr, AttendPlan{}, nullptr);
+    const dim3 grid(uint32_t(a.n_rows / 16 + kStoreUnits * a.n_seqs), uint32_t(a.Hkv));
+    hipStream_t st = as_stream(stream);
+    if (k->type == CARD_F32 && h == 128) hipLaunchKernelGGL((k_read4<128, float>), grid, dim3(256), 0, st, a);
+    else if (k->type == CARD_F32) hipLaunchKernelGGL((k_read4<64, float>), grid, dim3(256), 0, st, a);
+    else if (h == 128) hipLaunchKernelGGL((k_read4<128, __bf16>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_read4<64, __bf16>), grid, dim3(256), 0, st, a);
+    return launch_status();
+}
+
+size_t card_kv4_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch) {
+    if (!batch_ok(cfg, batch) || !batch_fits(cfg, batch) || batch->n_rows == 0) return 0;
+    return std::max(attend4_plan(cfg, batch, false).bytes, attend4_plan(cfg, batch, true).bytes);
+}
+
+int card_kv4_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
+                    const card_rows* v, const card_rows* out, const card_row_mask* mask, void* workspace_dev, void* stream) {
+    if (const int st = attend_refused(cfg, batch, layer, q, k, v, out, mask)) return st;
+    if (batch->n_rows == 0) return CARD_OK;
+    const AttendPlan plan = attend4_plan(cfg, batch, q->type == CARD_F32);
+    if (plan.bytes > 0 && (!workspace_dev || !aligned16(workspace_dev))) return CARD_EINVAL;
+    if (k)
+        if (const int st = append(cfg, batch, layer, 4, nullptr, nullptr, nullptr, k, v, stream)) return st;
+    const AttendArgs a = attend_args(cfg, batch, layer, 4, q, nullptr, nullptr, out, mask, plan, workspace_dev);
+    hipStream_t st = as_stream(stream);
+    const int h = cfg->head_dim;
+    if (q->type == CARD_F32) attend4_launch<float, 1>(a, plan, h, st);
+    else if (plan.tiles == 1) attend4_launch<__bf16, 1>(a, plan, h, st);
+    else attend4_launch<__bf16, 2>(a, plan, h, st);
+    return launch_status();
+}
+
+}  // extern "C"

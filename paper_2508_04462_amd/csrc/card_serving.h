@@ -1,0 +1,101 @@
+// What the entry points for several sequences share: argument checks, and a batch as the kernels take it.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "card.h"
+#include "card_attend.hip"
+
+namespace card {
+
+inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? CARD_OK : CARD_EDEVICE; }
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+inline size_t layer4_bytes(const card_model_cfg* cfg, int32_t n_pages) { return size_t(n_pages) * cfg->n_kv_heads * 9 * cfg->head_dim; }
+inline size_t layer_elems(const card_model_cfg* cfg, int32_t n_pages) { return size_t(n_pages) * cfg->n_kv_heads * 16 * cfg->head_dim; }
+
+inline bool rows_ok(const card_rows* r, int32_t type, int64_t least_stride) {
+    const int64_t unit = type == CARD_F32 ? 4 : 8;
+    return r && r->data && r->type == type && aligned16(r->data) && r->row_stride >= least_stride && r->head_stride >= least_stride &&
+           r->row_stride % unit == 0 && r->head_stride % unit == 0;
+}
+
+inline bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
+    return cfg_valid(cfg) && b && b->n_pages > 0 && b->n_seqs > 0 && b->table_pages > 0 && b->table_pages < (1 << 27) && b->n_rows >= 0 &&
+           b->max_new >= 0 && b->max_len >= 0;
+}
+
+// A launch has less than 2^32 threads in x: 2^24 workgroups of 256.  (units of 16 rows x heads, and of 16 new tokens)
+constexpr int64_t kMostGroups = int64_t(1) << 24;
+inline bool batch_fits(const card_model_cfg* cfg, const card_kv_batch* b) {
+    return int64_t(b->n_rows) * cfg->n_q_heads / 16 + int64_t(kStoreUnits) * b->n_seqs * cfg->n_kv_heads < kMostGroups;
+}
+
+struct AttendPlan {
+    int32_t tiles, units, cuts, cut_pages;
+    bool fused;
+    size_t bytes;
+};
+
+inline int layer_refused(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer) {
+    if (!batch_ok(cfg, batch)) return CARD_EINVAL;
+    if (!batch->k_pages || !batch->v_pages || !batch->block_tables || !batch->ctx_lens || !batch->row_starts) return CARD_EINVAL;
+    if (!aligned16(batch->k_pages) || !aligned16(batch->v_pages)) return CARD_EINVAL;
+    if (layer < 0 || layer >= cfg->n_layers) return CARD_ERANGE;
+    return batch_fits(cfg, batch) ? CARD_OK : CARD_ERANGE;
+}
+inline int attend_refused(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k, const card_rows* v,
+                   const card_rows* out, const card_row_mask* mask) {
+    if (const int st = layer_refused(cfg, batch, layer)) return st;
+    if (batch->n_rows == 0) return CARD_OK;
+    if (!q || !out || (q->type != CARD_BF16 && q->type != CARD_F32)) return CARD_EINVAL;
+    if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
+    if (k && (!rows_ok(k, q->type, 0) || !rows_ok(v, q->type, 0))) return CARD_EINVAL;
+    if (mask && (!mask->mask_dev || !mask->mask_base_dev || mask->words < 1 || mask->words > (1 << 25))) return CARD_EINVAL;
+    return CARD_OK;
+}
+
+// bits: of a value in the cache, 16 or 4.  Without a plan, what storing needs.
+inline AttendArgs attend_args(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, int bits, const card_rows* q, const card_rows* k,
+                       const card_rows* v, const card_rows* out, const card_row_mask* mask, const AttendPlan& plan, void* workspace_dev) {
+    AttendArgs a = {};
+    if (q) {
+        a.q = q->data;
+        a.q_row = q->row_stride;
+        a.q_head = q->head_stride;
+        a.out = out->data;
+        a.o_row = out->row_stride;
+        a.o_head = out->head_stride;
+    }
+    if (k) {
+        a.k = k->data;
+        a.k_row = k->row_stride;
+        a.k_head = k->head_stride;
+        a.v = v->data;
+        a.v_row = v->row_stride;
+        a.v_head = v->head_stride;
+    }
+    const size_t layer_bytes = bits == 16 ? 2 * layer_elems(cfg, batch->n_pages) : layer4_bytes(cfg, batch->n_pages);
+    a.kpool = reinterpret_cast<__bf16*>(static_cast<char*>(batch->k_pages) + size_t(layer) * layer_bytes);
+    a.vpool = reinterpret_cast<__bf16*>(static_cast<char*>(batch->v_pages) + size_t(layer) * layer_bytes);
+    a.tables = batch->block_tables;
+    a.ctx = batch->ctx_lens;
+    a.starts = batch->row_starts;
+    a.table_pages = batch->table_pages;
+    a.n_pages = batch->n_pages;
+    a.n_seqs = batch->n_seqs;
+    a.n_rows = batch->n_rows;
+    a.Hkv = cfg->n_kv_heads;
+    a.G = cfg->n_q_heads / cfg->n_kv_heads;
+    if (mask) {
+        a.mask = mask->mask_dev;
+        a.mask_base = mask->mask_base_dev;
+        a.mask_words = mask->words;
+    }
+    a.scale = 1.4426950408889634f / sqrtf(float(cfg->head_dim));
+    a.cuts = plan.cuts;
+    a.cut_pages = plan.cut_pages;
+    a.part = static_cast<float*>(workspace_dev);
+    return a;
+}
+
+}  // namespace card

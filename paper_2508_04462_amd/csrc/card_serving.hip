@@ -9,15 +9,11 @@
 #include "card_attend.hip"
 #include "card_logprobs.hip"
 #include "card_pages.hip"
+#include "card_serving.h"
 
 using namespace card;
 
 namespace {
-
-inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
-inline int launch_status() { return hipGetLastError() == hipSuccess ? CARD_OK : CARD_EDEVICE; }
-inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-inline size_t layer_elems(const card_model_cfg* cfg, int32_t n_pages) { return size_t(n_pages) * cfg->n_kv_heads * 16 * cfg->head_dim; }
 
 // A set of numbers >= 0, open addressing.
 class NumberSet {
@@ -55,23 +51,6 @@ int pool_args(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int
     if (n > 0 && (!src || !dst)) return CARD_EINVAL;
     if (!aligned16(kv->k_pages) || !aligned16(kv->v_pages)) return CARD_EINVAL;
     return CARD_OK;
-}
-
-bool rows_ok(const card_rows* r, int32_t type, int64_t least_stride) {
-    const int64_t unit = type == CARD_F32 ? 4 : 8;
-    return r && r->data && r->type == type && aligned16(r->data) && r->row_stride >= least_stride && r->head_stride >= least_stride &&
-           r->row_stride % unit == 0 && r->head_stride % unit == 0;
-}
-
-bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
-    return cfg_valid(cfg) && b && b->n_pages > 0 && b->n_seqs > 0 && b->table_pages > 0 && b->table_pages < (1 << 27) && b->n_rows >= 0 &&
-           b->max_new >= 0 && b->max_len >= 0;
-}
-
-// A launch has less than 2^32 threads in x: 2^24 workgroups of 256.  (units of 16 rows x heads, and of 16 new tokens)
-constexpr int64_t kMostGroups = int64_t(1) << 24;
-bool batch_fits(const card_model_cfg* cfg, const card_kv_batch* b) {
-    return int64_t(b->n_rows) * cfg->n_q_heads / 16 + int64_t(kStoreUnits) * b->n_seqs * cfg->n_kv_heads < kMostGroups;
 }
 
 template <int ROUND>
@@ -114,11 +93,6 @@ constexpr int kFill = 512;
 // 100; R = 512 behind 700 tokens 16.5 and 18.2, behind 2000 28.0 and 23.6; k_attend_many, R = 640 behind 100 17.9 and 18.9, behind 700 34 and 24, R = 2000 behind 300 33 and
 // 33, behind 500 39 and 35, behind 1500 67 and 46, R = 4000 behind 1000 69 and 71.)
 int64_t pages_uncut(int tiles, int64_t groups) { return tiles == kManyTiles ? 8 + groups / 2 : 32 + groups / 3; }
-struct AttendPlan {
-    int32_t tiles, units, cuts, cut_pages;
-    bool fused;
-    size_t bytes;
-};
 AttendPlan attend_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f32) {
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
@@ -150,6 +124,7 @@ template <typename T, int NT>
 void attend_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t st) {
     h == 128 ? attend_launch<128, T, NT>(a, p, st) : attend_launch<64, T, NT>(a, p, st);
 }
+
 
 }  // namespace
 
@@ -222,53 +197,11 @@ size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_b
 
 int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
                    const card_rows* v, const card_rows* out, const card_row_mask* mask, void* workspace_dev, void* stream) {
-    if (!batch_ok(cfg, batch)) return CARD_EINVAL;
-    if (!batch->k_pages || !batch->v_pages || !batch->block_tables || !batch->ctx_lens || !batch->row_starts) return CARD_EINVAL;
-    if (!aligned16(batch->k_pages) || !aligned16(batch->v_pages)) return CARD_EINVAL;
-    if (layer < 0 || layer >= cfg->n_layers) return CARD_ERANGE;
-    if (!batch_fits(cfg, batch)) return CARD_ERANGE;
+    if (const int st = attend_refused(cfg, batch, layer, q, k, v, out, mask)) return st;
     if (batch->n_rows == 0) return CARD_OK;
-    if (!q || !out || (q->type != CARD_BF16 && q->type != CARD_F32)) return CARD_EINVAL;
-    if (!rows_ok(q, q->type, 0) || !rows_ok(out, q->type, cfg->head_dim) || !k != !v) return CARD_EINVAL;
-    if (k && (!rows_ok(k, q->type, 0) || !rows_ok(v, q->type, 0))) return CARD_EINVAL;
-    if (mask && (!mask->mask_dev || !mask->mask_base_dev || mask->words < 1 || mask->words > (1 << 25))) return CARD_EINVAL;
     const AttendPlan plan = attend_plan(cfg, batch, q->type == CARD_F32);
     if (plan.bytes > 0 && (!workspace_dev || !aligned16(workspace_dev))) return CARD_EINVAL;
-    AttendArgs a = {};
-    a.q = q->data;
-    a.q_row = q->row_stride;
-    a.q_head = q->head_stride;
-    if (k) {
-        a.k = k->data;
-        a.k_row = k->row_stride;
-        a.k_head = k->head_stride;
-        a.v = v->data;
-        a.v_row = v->row_stride;
-        a.v_head = v->head_stride;
-    }
-    a.out = out->data;
-    a.o_row = out->row_stride;
-    a.o_head = out->head_stride;
-    a.kpool = static_cast<__bf16*>(batch->k_pages) + size_t(layer) * layer_elems(cfg, batch->n_pages);
-    a.vpool = static_cast<__bf16*>(batch->v_pages) + size_t(layer) * layer_elems(cfg, batch->n_pages);
-    a.tables = batch->block_tables;
-    a.ctx = batch->ctx_lens;
-    a.starts = batch->row_starts;
-    a.table_pages = batch->table_pages;
-    a.n_pages = batch->n_pages;
-    a.n_seqs = batch->n_seqs;
-    a.n_rows = batch->n_rows;
-    a.Hkv = cfg->n_kv_heads;
-    a.G = cfg->n_q_heads / cfg->n_kv_heads;
-    if (mask) {
-        a.mask = mask->mask_dev;
-        a.mask_base = mask->mask_base_dev;
-        a.mask_words = mask->words;
-    }
-    a.scale = 1.4426950408889634f / sqrtf(float(cfg->head_dim));
-    a.cuts = plan.cuts;
-    a.cut_pages = plan.cut_pages;
-    a.part = static_cast<float*>(workspace_dev);
+    const AttendArgs a = attend_args(cfg, batch, layer, 16, q, k, v, out, mask, plan, workspace_dev);
     hipStream_t st = as_stream(stream);
     const int h = cfg->head_dim;
     if (q->type == CARD_F32) attend_launch<float, 1>(a, plan, h, st);
