@@ -581,6 +581,10 @@ size_t card_kv4_pool_bytes(const card_model_cfg* cfg, int32_t n_pages);
 int card_kv4_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
                     const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream);
 int card_kv4_read(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* k, const card_rows* v, void* stream);
+int card_kv4_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host,
+                        const int32_t* dst_host, void* stream);
+int card_kv4_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host,
+                        const int32_t* dst_host, void* stream);
 size_t card_kv4_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch);
 int card_kv4_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rows* q, const card_rows* k,
                     const card_rows* v, const card_rows* out, const card_row_mask* mask, void* workspace_dev, void* stream);
@@ -602,6 +606,35 @@ size_t card_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vocab, int64_t row_stride,
                   const int32_t* tokens_dev, float temperature, int32_t top, float* logprob_dev, float* entropy_dev,
                   int32_t* top_tokens_dev, float* top_logprobs_dev, void* workspace_dev, void* stream);
+
+/* Beam search, one step: of each of `groups` searches, the out_beams best continuations of its beams.  A candidate is a beam and a token of the vocabulary, its score the beam's
+ * score + ln softmax(logits / temperature) of the token; a beam that has ended has one candidate, itself, with its score and eos_token.  Candidates are
+ * compared in 64 bits; equal scores go by beam, then by token.  Row group * beams + beam of logits_dev belongs to a beam; those of beams that have ended are not
+ * read.  The histories of the beams move with them: out_history of a new beam is that of its parent, lengths[group] tokens, and then its token
+ * (where there is room for it; what lies behind is not touched).
+ *   logits_dev, type, vocab, row_stride, temperature: as card_logprobs
+ *   workspace_dev: card_beam_select_workspace_bytes, 16-byte aligned, no preparation; calls that may run at the same time do not share one
+ * A logit of -inf is no candidate, a beam whose score is not finite has none, and neither has one with a NaN or +inf among its logits.  Where there are fewer
+ * candidates than out_beams, the beams behind them have score -inf, token -1, parent 0 and have ended; their histories are not written.
+ * Outputs overlap no input.  out_beams may differ from beams (a search begins with one).
+ * Errors: CARD_EINVAL, CARD_ERANGE (beams or out_beams outside [1, 32]; groups * beams >= 2^24; vocab >= 2^30; eos_token), CARD_EDEVICE. */
+typedef struct card_beams {
+    int32_t groups, beams, out_beams;
+    int32_t eos_token;           /* a beam that takes it has ended; -1: none                                      */
+    const float* scores_dev;     /* [groups][beams]: sums of log probabilities; -inf: no beam                      */
+    const int32_t* done_dev;     /* [groups][beams], not 0: ended; NULL: none has                                  */
+    const int32_t* history_dev;  /* [groups][beams][history_len], or NULL                                          */
+    const int32_t* lengths_dev;  /* [groups], taken as in [0, history_len]                                         */
+    int32_t history_len;
+    float* out_scores_dev;       /* [groups][out_beams], best first                                                */
+    int32_t* out_tokens_dev;
+    int32_t* out_parents_dev;    /* beams of the group                                                             */
+    int32_t* out_done_dev;       /* or NULL                                                                        */
+    int32_t* out_history_dev;    /* [groups][out_beams][history_len], with history_dev                             */
+} card_beams;
+size_t card_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t out_beams, int32_t vocab);
+int card_beam_select(const void* logits_dev, int32_t type, int32_t vocab, int64_t row_stride, const card_beams* beams, float temperature,
+                     void* workspace_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -78,6 +78,15 @@ class CardRotation(C.Structure):
     _fields_ = [("freqs_host", C.c_void_p), ("positions_dev", C.c_void_p)]
 
 
+class CardBeams(C.Structure):
+    _fields_ = [
+        ("groups", C.c_int32), ("beams", C.c_int32), ("out_beams", C.c_int32), ("eos_token", C.c_int32),
+        ("scores_dev", C.c_void_p), ("done_dev", C.c_void_p), ("history_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("history_len", C.c_int32),
+        ("out_scores_dev", C.c_void_p), ("out_tokens_dev", C.c_void_p), ("out_parents_dev", C.c_void_p), ("out_done_dev", C.c_void_p),
+        ("out_history_dev", C.c_void_p),
+    ]
+
+
 class CardSampling(C.Structure):
     _fields_ = [("temperature", C.c_float), ("seed", C.c_uint64)]
 
@@ -169,7 +178,7 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.card_verify_debug_logits.argtypes = [_cfgp, _P, _kvp, C.c_int32, _P, C.c_int32, _P, _P, _P, _P, _P]
     lib.card_kv_gather.restype = C.c_int
     lib.card_kv_gather.argtypes = [_cfgp, _kvp, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]
-    for _n in ("card_kv_copy_pages", "card_kv_move_slots"):
+    for _n in ("card_kv_copy_pages", "card_kv_move_slots", "card_kv4_copy_pages", "card_kv4_move_slots"):
         getattr(lib, _n).restype = C.c_int
         getattr(lib, _n).argtypes = [_cfgp, _kvp, C.c_int32, _i32p, _i32p, _P]
     _rowsp = C.POINTER(CardRows)
@@ -192,6 +201,10 @@ def _declare(lib: C.CDLL) -> C.CDLL:
     lib.card_logprobs_workspace_bytes.argtypes = [C.c_int32] * 3
     lib.card_logprobs.restype = C.c_int
     lib.card_logprobs.argtypes = [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_float, C.c_int32] + [_P] * 6
+    lib.card_beam_select_workspace_bytes.restype = C.c_size_t
+    lib.card_beam_select_workspace_bytes.argtypes = [C.c_int32] * 4
+    lib.card_beam_select.restype = C.c_int
+    lib.card_beam_select.argtypes = [_P, C.c_int32, C.c_int32, C.c_int64, C.POINTER(CardBeams), C.c_float, _P, _P]
     lib.card_profile_enable.restype = C.c_int
     lib.card_profile_enable.argtypes = [C.c_int32]
     lib.card_profile_disable.restype = C.c_int
@@ -398,6 +411,18 @@ def card_kv_move_slots(cfg, kv: CardKV, src_slots, dst_slots, stream=None) -> in
     return lib.card_kv_move_slots(cfg, kv, len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
 
 
+def card_kv4_copy_pages(cfg, kv: CardKV, src_pages, dst_pages, stream=None) -> int:
+    if len(src_pages) != len(dst_pages):
+        return CARD_EINVAL
+    return lib.card_kv4_copy_pages(cfg, kv, len(src_pages), _i32(src_pages), _i32(dst_pages), _ptr(stream))
+
+
+def card_kv4_move_slots(cfg, kv: CardKV, src_slots, dst_slots, stream=None) -> int:
+    if len(src_slots) != len(dst_slots):
+        return CARD_EINVAL
+    return lib.card_kv4_move_slots(cfg, kv, len(src_slots), _i32(src_slots), _i32(dst_slots), _ptr(stream))
+
+
 _TYPES = {}
 
 
@@ -486,6 +511,21 @@ def card_logprobs(logits, tokens_dev, temperature: float, top: int, logprob_dev,
     return lib.card_logprobs(logits.data_ptr(), _type(logits), rows, vocab, row if rows > 1 else vocab, _ptr(tokens_dev),
                              temperature, top, _ptr(logprob_dev), _ptr(entropy_dev), _ptr(top_tokens_dev), _ptr(top_logprobs_dev),
                              _ptr(workspace_dev), _ptr(stream))
+
+
+def card_beam_select_workspace_bytes(groups: int, beams: int, out_beams: int, vocab: int) -> int:
+    return lib.card_beam_select_workspace_bytes(groups, beams, out_beams, vocab)
+
+
+def card_beam_select(logits, beams: CardBeams, temperature: float, workspace_dev, stream=None) -> int:
+    """logits: a tensor [groups * beams][vocab] whose last dimension is contiguous."""
+    rows, vocab = logits.shape
+    row, one = logits.stride()
+    if vocab > 1 and one != 1:
+        raise ValueError("the logits of a row have to lie side by side")
+    if rows != beams.groups * beams.beams:
+        return CARD_EINVAL
+    return lib.card_beam_select(logits.data_ptr(), _type(logits), vocab, row if rows > 1 else vocab, beams, temperature, _ptr(workspace_dev), _ptr(stream))
 
 
 def card_profile_enable(max_launches: int) -> int:

@@ -10,7 +10,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libcard.so")
 SOURCES = [
     os.path.join(PKG_DIR, "csrc", "card_api.hip"),
     os.path.join(PKG_DIR, "csrc", "card_serving.hip"),
-    os.path.join(PKG_DIR, "csrc", "card_cache4.hip"),
+    os.path.join(PKG_DIR, "csrc", "card_sequences.hip"),
     os.path.join(PKG_DIR, "csrc", "card_cache.cpp"),
 ]
 

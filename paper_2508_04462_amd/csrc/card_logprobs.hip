@@ -184,13 +184,12 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, const LogprobSh
     }
 }
 
-// One workgroup: one part of one row, in turns of kLpVecs 16-byte loads a lane.  The loads are of aligned units, whatever the row begins at:
+// A workgroup's part of a row, in turns of kLpVecs 16-byte loads a lane: returns its sums, and leaves its most probable tokens in sm.out.  The loads are of aligned units, whatever the row begins at:
 // what a unit holds before the row or behind it is not read.
 template <typename T>
-__global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
+__device__ __forceinline__ RowSums scan_part(const LogprobArgs& a, LogprobShared& sm, int row, int part) {
     constexpr int VN = 16 / sizeof(T);
-    __shared__ LogprobShared sm;
-    const int row = blockIdx.x, part = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float c = a.inv_temp * kLog2e;
     const T* x0 = static_cast<const T*>(a.logits) + int64_t(row) * a.row_stride;
@@ -259,14 +258,23 @@ __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
             if (lane == 0 && list.least > before) atomicMax(&sm.least, list.least);
         }
     }
-    r = join_waves(sm, r, list, a.top, c);
-    if (a.parts == 1) {
-        finish_row<T>(a, sm, r, row);
-        return;
-    }
+    return join_waves(sm, r, list, a.top, c);
+}
+__device__ __forceinline__ void leave_part(const LogprobArgs& a, const LogprobShared& sm, RowSums r, int row, int part) {
+    const int tid = threadIdx.x;
     const size_t at = size_t(row) * a.parts + part;
     if (tid == 0) *reinterpret_cast<floatx4*>(a.part_sums + at * 4) = floatx4{r.m, r.s, r.t, 0.f};
     if (tid < a.top) a.part_keys[at * a.top + tid] = sm.out[tid];
+}
+
+// One workgroup: one part of one row.
+template <typename T>
+__global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
+    __shared__ LogprobShared sm;
+    const int row = blockIdx.x, part = blockIdx.y;
+    const RowSums r = scan_part<T>(a, sm, row, part);
+    if (a.parts == 1) finish_row<T>(a, sm, r, row);
+    else leave_part(a, sm, r, row, part);
 }
 
 // One workgroup: the parts of a row.

@@ -1,6 +1,6 @@
 // Page copies and slot moves inside the page pools.
 #pragma once
-#include "card_common.hip"
+#include "card_append.hip"
 
 namespace card {
 
@@ -127,6 +127,47 @@ __global__ __launch_bounds__(H / 64 * 192) void k_kv_move_slots(MoveArgs a) {
                     if (i + at + e < end && to[e] >= 0) *place(to[e]) = w[r + e];
             }
         });
+}
+
+// The same in pages of 4 bits a value (Page4).  One workgroup: one head of one layer, a wavefront for K and one for V; a lane owns a piece of a token for all moves (K: a word, V: the
+// two bytes of four channels, and the words behind the codes), and all of a round is read before any is written, which is the order of the list, as above.  1500 tokens of 32
+// layers x 8 heads x 128: MOVED.
+constexpr int kMoveRound4 = 32;  // loads of a lane
+template <int H>
+__global__ __launch_bounds__(128) void k_kv4_move_slots(MoveArgs a) {
+    using P = Page4<H>;
+    constexpr int G = H / 64, R = kMoveRound4;
+    const int head = blockIdx.x, lane = threadIdx.x & 63, first = blockIdx.z * a.part, end = min(a.n, first + a.part);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const auto rounds = [&](auto per, int sub, bool owns, auto&& read, auto&& write) {  // per: moves of a load
+        constexpr int PER = decltype(per)::value;
+        for (int i = first; i < end; i += R * PER) {
+            uint32_t v[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) v[r] = read(a.src[min(i + r * PER + sub, end - 1)]);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (owns && i + r * PER + sub < end) write(a.dst[i + r * PER + sub], v[r]);
+        }
+    };
+    char* pool = reinterpret_cast<char*>((wave == 0 ? a.kpool : a.vpool) + blockIdx.y * a.layer_elems);
+    const auto page_at = [&](int slot) { return pool + P::at(slot >> 4, a.n_kv_heads, head); };
+    if (wave == 0) {
+        constexpr int SLOTS = H / 4;
+        const int piece = min(lane % SLOTS, H / 8 + G - 1);
+        const auto word = [&](int slot) { return reinterpret_cast<uint32_t*>(page_at(slot)) + (piece < H / 8 ? P::k_word(piece, slot & 15) : P::word(piece - H / 8, slot & 15)); };
+        rounds(std::integral_constant<int, 64 / SLOTS>{}, lane / SLOTS, lane % SLOTS < H / 8 + G, [&](int slot) { return *word(slot); }, [&](int slot, uint32_t v) { *word(slot) = v; });
+        return;
+    }
+    constexpr int SLOTS = H / 2;
+    const int piece = min(lane % SLOTS, 17 * G - 1);
+    const auto half = [&](int slot) { return reinterpret_cast<unsigned short*>(page_at(slot)) + P::v_half(piece & 15, piece >> 4, slot & 15); };
+    const auto word = [&](int slot) { return reinterpret_cast<uint32_t*>(page_at(slot)) + P::word(piece - 16 * G, slot & 15); };
+    rounds(std::integral_constant<int, 64 / SLOTS>{}, lane / SLOTS, lane % SLOTS < 17 * G, [&](int slot) { return piece < 16 * G ? uint32_t(*half(slot)) : *word(slot); },
+           [&](int slot, uint32_t v) {
+               if (piece < 16 * G) *half(slot) = static_cast<unsigned short>(v);
+               else *word(slot) = v;
+           });
 }
 
 }  // namespace card

@@ -1,4 +1,4 @@
-// C ABI of rotation with storing, and of the cache of 4 bits a value: argument checks and launches.
+// C ABI of rotation with storing, of the cache of 4 bits a value and of the selection of beams: argument checks and launches.
 #include <algorithm>
 #include <cmath>
 #include <hip/hip_runtime.h>
@@ -6,6 +6,7 @@
 #include "card.h"
 #include "card_append.hip"
 #include "card_attend4.hip"
+#include "card_beams.hip"
 #include "card_serving.h"
 
 using namespace card;
@@ -85,7 +86,7 @@ int card_kv_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
 }
 
 size_t card_kv4_pool_bytes(const card_model_cfg* cfg, int32_t n_pages) {
-    return cfg_valid(cfg) && n_pages > 0 ? size_t(cfg->n_layers) * layer4_bytes(cfg, n_pages) : 0;
+    return cfg_valid(cfg) && n_pages > 0 ? size_t(cfg->n_layers) * layer_bytes(cfg, n_pages, 4) : 0;
 }
 
 int card_kv4_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, const card_rotation* rotation, const card_rows* q,
@@ -127,6 +128,59 @@ int card_kv4_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32
     if (q->type == CARD_F32) attend4_launch<float, 1>(a, plan, h, st);
     else if (plan.tiles == 1) attend4_launch<__bf16, 1>(a, plan, h, st);
     else attend4_launch<__bf16, 2>(a, plan, h, st);
+    return launch_status();
+}
+
+size_t card_beam_select_workspace_bytes(int32_t groups, int32_t beams, int32_t out_beams, int32_t vocab) {
+    if (groups < 1 || beams < 1 || beams > kMostBeams || out_beams < 1 || out_beams > kMaxTop || vocab < 1 || vocab >= kMostLogits) return 0;
+    if (int64_t(groups) * beams >= kMostGroups) return 0;
+    // (r rows have at most r + 767 parts: enough for fewer groups, too)
+    const int64_t rows = int64_t(groups) * beams, parts = std::min(rows * ceil_div(vocab, 4096), rows + 768);
+    return size_t(parts) * (16 + 8 * size_t(out_beams));
+}
+
+int card_beam_select(const void* logits_dev, int32_t type, int32_t vocab, int64_t row_stride, const card_beams* beams, float temperature,
+                     void* workspace_dev, void* stream) {
+    if (!beams || (type != CARD_BF16 && type != CARD_F32) || vocab < 1 || row_stride < vocab) return CARD_EINVAL;
+    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return CARD_EINVAL;
+    if (beams->groups < 0 || beams->history_len < 0) return CARD_EINVAL;
+    if (beams->beams < 1 || beams->beams > kMostBeams || beams->out_beams < 1 || beams->out_beams > kMaxTop || vocab >= kMostLogits) return CARD_ERANGE;
+    if (int64_t(beams->groups) * beams->beams >= kMostGroups || beams->eos_token < -1 || beams->eos_token >= vocab) return CARD_ERANGE;
+    if (beams->groups == 0) return CARD_OK;
+    if (!logits_dev || !beams->scores_dev || !beams->out_scores_dev || !beams->out_tokens_dev || !beams->out_parents_dev) return CARD_EINVAL;
+    if (beams->history_dev && (!beams->lengths_dev || !beams->out_history_dev)) return CARD_EINVAL;
+    if (!workspace_dev || !aligned16(workspace_dev)) return CARD_EINVAL;
+    const int rows = beams->groups * beams->beams, parts = logprob_parts(rows, vocab);
+    BeamArgs b = {};
+    LogprobArgs& a = b.rows;
+    a.logits = logits_dev;
+    a.row_stride = row_stride;
+    a.vocab = vocab;
+    a.top = beams->out_beams;
+    a.inv_temp = 1.0f / temperature;
+    const int units = vocab / (type == CARD_F32 ? 4 : 8) + 2;  // of 16 bytes, the ends of a row that begins anywhere among them
+    a.part_vecs = ceil_div(units, parts);
+    a.parts = ceil_div(units, a.part_vecs);
+    a.part_sums = static_cast<float*>(workspace_dev);
+    a.part_keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace_dev) + logprob_sums_bytes(rows, vocab));
+    b.beams = beams->beams;
+    b.eos = beams->eos_token;
+    b.history_len = beams->history_len;
+    b.temperature = temperature;
+    b.scores = beams->scores_dev;
+    b.done = beams->done_dev;
+    b.history = beams->history_len > 0 ? beams->history_dev : nullptr;
+    b.lengths = beams->lengths_dev;
+    b.out_scores = beams->out_scores_dev;
+    b.out_tokens = beams->out_tokens_dev;
+    b.out_parents = beams->out_parents_dev;
+    b.out_done = beams->out_done_dev;
+    b.out_history = beams->out_history_dev;
+    const dim3 grid(static_cast<uint32_t>(rows), uint32_t(a.parts));
+    hipStream_t st = as_stream(stream);
+    if (type == CARD_F32) hipLaunchKernelGGL(k_beam_rows<float>, grid, dim3(kLpThreads), 0, st, b);
+    else hipLaunchKernelGGL(k_beam_rows<__bf16>, grid, dim3(kLpThreads), 0, st, b);
+    hipLaunchKernelGGL(k_beam_join, dim3(uint32_t(beams->groups)), dim3(64 * uint32_t(std::min(std::max(beams->beams, 4), 16))), 0, st, b);
     return launch_status();
 }
 

@@ -59,14 +59,6 @@ void move_launch(const MoveArgs& a, int h, dim3 grid, hipStream_t st) {
     else hipLaunchKernelGGL((k_kv_move_slots<64, ROUND>), grid, dim3(192), 0, st, a);
 }
 
-// How a row of logits is cut: one workgroup per row where the rows fill the GPU, else parts of 4096 logits or more (one row of 128256 in fp32 in parts
-// of 1024, 4096, 16384 or whole 9.5, 9.2, 12.2, 26 us, eight 10.2, 9.3, 13.0, 28).  1000 rows of 152064 in bf16,
-// the most probable token: for 512, 768, 1024 or 2048 workgroups 54.7, 55.1, 59.4, 67.4 us; 300 rows 28.6, 27.6, 26.8, 30.1; 100 of 128256 in fp32
-// 16.5, 15.8, 15.8, 17.7.
-int32_t logprob_parts(int32_t rows, int32_t vocab) { return std::min(ceil_div(vocab, 4096), ceil_div(768, rows)); }
-constexpr int32_t kMostLogits = 1 << 30;  // of a row: they are counted in 32 bits, with the rest of a 16-byte unit at either end
-size_t logprob_sums_bytes(int32_t rows, int32_t vocab) { return size_t(rows) * logprob_parts(rows, vocab) * 16; }
-
 template <typename T>
 int logprobs_launch(const LogprobArgs& a, int32_t rows, hipStream_t st) {
     hipLaunchKernelGGL(k_logprobs<T>, dim3(uint32_t(rows), uint32_t(a.parts)), dim3(kLpThreads), 0, st, a);
@@ -125,13 +117,8 @@ void attend_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t 
     h == 128 ? attend_launch<128, T, NT>(a, p, st) : attend_launch<64, T, NT>(a, p, st);
 }
 
-
-}  // namespace
-
-extern "C" {
-
-int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
-                       void* stream) {
+// bits: of a value in the pages, 16 or 4.
+int copy_pages(const card_model_cfg* cfg, const card_kv* kv, int bits, int32_t n, const int32_t* src_host, const int32_t* dst_host, void* stream) {
     if (const int st = pool_args(cfg, kv, n, src_host, dst_host)) return st;
     if (n == 0) return CARD_OK;
     NumberSet written(n);
@@ -145,8 +132,8 @@ int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
     CopyArgs a = {};
     a.pool[0] = static_cast<uint4v*>(kv->k_pages);
     a.pool[1] = static_cast<uint4v*>(kv->v_pages);
-    a.layer16 = layer_elems(cfg, kv->n_pages) / 8;
-    a.page16 = cfg->n_kv_heads * 2 * cfg->head_dim;
+    a.layer16 = layer_bytes(cfg, kv->n_pages, bits) / 16;
+    a.page16 = int32_t(layer_bytes(cfg, 1, bits) / 16);
     for (int i = 0; i < n; i += kCopyPairs) {
         const int m = std::min(n - i, kCopyPairs);
         std::copy(src_host + i, src_host + i + m, a.src);
@@ -156,8 +143,7 @@ int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
     return launch_status();
 }
 
-int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
-                       void* stream) {
+int move_slots(const card_model_cfg* cfg, const card_kv* kv, int bits, int32_t n, const int32_t* src_host, const int32_t* dst_host, void* stream) {
     if (const int st = pool_args(cfg, kv, n, src_host, dst_host)) return st;
     if (n == 0) return CARD_OK;
     NumberSet written(n);
@@ -172,22 +158,48 @@ int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, 
     MoveArgs a = {};
     a.kpool = static_cast<__bf16*>(kv->k_pages);
     a.vpool = static_cast<__bf16*>(kv->v_pages);
-    a.layer_elems = layer_elems(cfg, kv->n_pages);
+    a.layer_elems = layer_bytes(cfg, kv->n_pages, bits) / 2;
     a.n_kv_heads = cfg->n_kv_heads;
     for (int i = 0; i < n;) {
         for (a.n = 0; i < n && a.n < kMoveSlots; ++a.n) {
             const int32_t* d = dst_host + i;
-            const bool four = i + 4 <= n && d[1] == d[0] + 1 && d[2] == d[0] + 2 && d[3] == d[0] + 3;
+            const bool four = bits == 16 && i + 4 <= n && d[1] == d[0] + 1 && d[2] == d[0] + 2 && d[3] == d[0] + 3;
             a.src[a.n] = src_host[i];
             a.dst[a.n] = four && (d[0] - a.n) % 4 != 0 ? -1 : d[0];
             i += a.dst[a.n] >= 0;
         }
         a.part = apart ? kMoveApart : kMoveSlots;
         const dim3 grid(uint32_t(cfg->n_kv_heads), uint32_t(cfg->n_layers), uint32_t(ceil_div(a.n, a.part)));
-        if (apart || a.n <= 7 * kMoveShort) move_launch<kMoveShort>(a, cfg->head_dim, grid, as_stream(stream));
+        if (bits == 4 && cfg->head_dim == 128) hipLaunchKernelGGL(k_kv4_move_slots<128>, grid, dim3(128), 0, as_stream(stream), a);
+        else if (bits == 4) hipLaunchKernelGGL(k_kv4_move_slots<64>, grid, dim3(128), 0, as_stream(stream), a);
+        else if (apart || a.n <= 7 * kMoveShort) move_launch<kMoveShort>(a, cfg->head_dim, grid, as_stream(stream));
         else move_launch<kMoveRound>(a, cfg->head_dim, grid, as_stream(stream));
     }
     return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int card_kv_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                       void* stream) {
+    return copy_pages(cfg, kv, 16, n, src_host, dst_host, stream);
+}
+
+int card_kv_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                       void* stream) {
+    return move_slots(cfg, kv, 16, n, src_host, dst_host, stream);
+}
+
+int card_kv4_copy_pages(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                        void* stream) {
+    return copy_pages(cfg, kv, 4, n, src_host, dst_host, stream);
+}
+
+int card_kv4_move_slots(const card_model_cfg* cfg, const card_kv* kv, int32_t n, const int32_t* src_host, const int32_t* dst_host,
+                        void* stream) {
+    return move_slots(cfg, kv, 4, n, src_host, dst_host, stream);
 }
 
 size_t card_kv_attend_workspace_bytes(const card_model_cfg* cfg, const card_kv_batch* batch) {

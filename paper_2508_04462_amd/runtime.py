@@ -151,6 +151,8 @@ class Target:
             a, b = self.cfg, pool.cfg
             if (a.n_layers, a.n_kv_heads, a.head_dim) != (b.n_layers, b.n_kv_heads, b.head_dim) or pool.device != self.k_pages.device:
                 raise ValueError("a pool of other layers or heads, or on another device")
+            if pool.bits != 16:
+                raise ValueError("a pool of 4 bits: steps and prompts run on 16")
             if b.max_ctx < a.max_ctx:  # calls may look at as many places of the block table
                 raise ValueError("a pool of shorter sequences")
             pool.length(seq)  # (an unknown sequence raises here)

@@ -348,3 +348,52 @@ def test_attend4_precision(dtype):
         torch.cuda.synchronize()
         off = float((c.out.cpu().double() - out).norm() / out.norm())
         assert off <= (1.75e-3 if dtype == BF16 else 2e-6), off
+
+
+def _pools4(pages, heads, h, layers=3, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randint(0, 256, (layers, pages, heads, 9 * h), generator=g, dtype=torch.uint8) for _ in range(2)]
+
+
+def _token(pool, values_, slot, h):
+    """The nibbles and words of a slot, [layers][heads][..]."""
+    page = pool[:, slot // PAGE]
+    nibbles = torch.stack((page & 15, page >> 4), -1).flatten(-2)[..., (k_nibbles if values_ == "k" else v_nibbles)(torch.tensor([slot % PAGE]), h)[0]]
+    words = page.contiguous().view(torch.int32)[..., 2 * h + torch.arange(h // 64) * PAGE + slot % PAGE]
+    return nibbles.clone(), words.clone()
+
+
+def _put_token(pool, values_, slot, h, token):
+    for layer in range(pool.shape[0]):
+        put_tokens(pool[layer], slot // PAGE, torch.tensor([slot % PAGE]), token[0][layer][None].long(), token[1][layer][None],
+                   k_nibbles if values_ == "k" else v_nibbles)
+
+
+@pytest.mark.parametrize("h,heads", [(64, 2), (128, 3)])
+def test_copy_pages_and_move_slots_of_4_bits(h, heads):
+    import paper_2508_04462_amd as card
+
+    cfg, n_pages = _cfg((heads, heads, h), 3), 300
+    g = torch.Generator().manual_seed(1)
+    lists = [([3, 4, 9], [1, 2, 5]), ([299], [0]), (list(range(0, 300, 2))[:150], list(range(1, 300, 2))[:150])]
+    for src, dst in lists:
+        k, v = _pools4(n_pages, heads, h)
+        kd, vd = k.cuda(), v.cuda()
+        assert card.card_kv4_copy_pages(cfg, card.CardKV(kd.data_ptr(), vd.data_ptr(), None, n_pages, -1), src, dst, None) == card.CARD_OK
+        torch.cuda.synchronize()
+        for got, want in ((kd, k), (vd, v)):
+            want[:, dst] = want[:, src]
+            assert torch.equal(got.cpu(), want)
+    closing = sorted(torch.randperm(900, generator=g)[:600].tolist())  # gaps that close: in order
+    apart = torch.randperm(n_pages * 16, generator=g)[:140].tolist()
+    moves = [([5], [7]), ([17, 33, 20], [3, 4, 31]), (apart[:70], apart[70:]), ([s + 5 for s in closing], list(range(5, 605))), (apart[:33], apart[100:133])]
+    for src, dst in moves:
+        src, dst = zip(*[(s, d) for s, d in zip(src, dst) if s != d])
+        k, v = _pools4(n_pages, heads, h, seed=2)
+        kd, vd = k.cuda(), v.cuda()
+        assert card.card_kv4_move_slots(cfg, card.CardKV(kd.data_ptr(), vd.data_ptr(), None, n_pages, -1), src, dst, None) == card.CARD_OK
+        torch.cuda.synchronize()
+        for s, d in zip(src, dst):
+            _put_token(k, "k", d, h, _token(k, "k", s, h))
+            _put_token(v, "v", d, h, _token(v, "v", s, h))
+        assert torch.equal(kd.cpu(), k) and torch.equal(vd.cpu(), v)
