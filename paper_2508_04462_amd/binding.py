@@ -439,8 +439,9 @@ def card_rows(t) -> CardRows:
     row, head, one = t.stride()
     if one != 1:
         raise ValueError("the elements of a head have to lie side by side")
+    kind = _TYPES.get(t.dtype)
     # (the stride of a dimension of one says nothing)
-    return CardRows(t.data_ptr(), _type(t), row if rows > 1 else heads * h, head if heads > 1 else h)
+    return CardRows(t.data_ptr(), _type(t) if kind is None else kind, row if rows > 1 else heads * h, head if heads > 1 else h)
 
 
 def card_kv_attend_workspace_bytes(cfg, batch: CardKVBatch) -> int:

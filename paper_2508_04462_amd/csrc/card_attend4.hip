@@ -8,13 +8,33 @@
 
 namespace card {
 
-// 16 + c of the codes in bits 4 R .. + 3 of either half of a word, as bf16.
-template <int R>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    return ((R == 0 ? w << 3 : w >> (4 * R - 3)) & 0x00780078u) | 0x41804180u;
-}
-__device__ __forceinline__ uint4v code_pairs(uint32_t w) { return uint4v{code_pair<0>(w), code_pair<1>(w), code_pair<2>(w), code_pair<3>(w)}; }
-
+// Numbers that are kept from the compiler: it would write the first two into two instructions where registers make one, and the third as a constant that the product takes
+// for another one.
+struct InRegisters {
+    uint32_t mask = 0x00780078u, sixteen = 0x41804180u, minus_first = 0x0000bf80u, minus_second = 0xbf800000u;
+    __device__ __forceinline__ InRegisters() { asm("" : "+s"(mask), "+v"(sixteen), "+s"(minus_first), "+s"(minus_second)); }
+    // 16 + c of the codes in bits 4 R .. + 3 of either half of a word, as bf16.
+    template <int R>
+    __device__ __forceinline__ uint32_t pair(uint32_t w) const {
+        return ((R == 0 ? w << 3 : w >> (4 * R - 3)) & mask) | sixteen;
+    }
+    __device__ __forceinline__ uint4v pairs(uint32_t w) const { return uint4v{pair<0>(w), pair<1>(w), pair<2>(w), pair<3>(w)}; }
+    // Two floats as sums of N bf16, as split_pair gives them: what the first part leaves comes out of a product with it, (-1, 0) and (0, -1), exact and an instruction each.
+    template <int N>
+    __device__ __forceinline__ void split(float x0, float x1, uint32_t (&p)[N]) const {
+        typedef __attribute__((ext_vector_type(2))) float float2v;
+        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bf16x2 part = __builtin_convertvector((float2v{x0, x1}), bf16x2);
+            p[i] = __builtin_bit_cast(uint32_t, part);
+            if (i + 1 < N) {
+                x0 = __builtin_amdgcn_fdot2_f32_bf16(part, __builtin_bit_cast(bf16x2, minus_first), x0, false);
+                x1 = __builtin_amdgcn_fdot2_f32_bf16(part, __builtin_bit_cast(bf16x2, minus_second), x1, false);
+            }
+        }
+    }
+};
 __device__ __forceinline__ uint32_t centred(uint32_t pair) {  // less 24: c - 8
     const float x = __uint_as_float(pair << 16) - 24.f, y = __uint_as_float(pair & 0xffff0000u) - 24.f;
     return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
@@ -74,23 +94,66 @@ __device__ __forceinline__ void query_sums(const bf16x8 (&qf)[NP][H / 32], float
         qs[g] = sum_across_rows(s);
     }
 }
-// The score of token 4 kq + e from the products of its groups.
-template <int H, int E>
-__device__ __forceinline__ float score_of(const floatx4 (&acc)[H / 64], const float (&qs)[H / 64], uint32_t scales, uint32_t offsets) {
-    float s = 0.f;
-    each<H / 64>([&](auto g) {
-        constexpr int AT = word_lane<H>(0, decltype(g)::value, E);
-        s = fmaf(row_lane<AT>(scales), acc[g][E], s);
-        s = fmaf(row_lane<AT>(offsets), qs[g], s);
-    });
-    return s;
+// The scores of tokens 4 kq .. + 3 from the products of their groups; and weights times scales, and times offsets, of tokens 4 kq .. + 3 and one group.  Broadcasts are operands
+// of the instructions, which the compiler makes moves of: 16 instructions instead of 32 a page.  (The compiler does not count for them: what is broadcast must be two
+// instructions old, a matrix instruction of four passes has its result after 8 and has read its registers after 3.)
+template <int H>
+__device__ __forceinline__ void scores_of(const floatx4 (&acc)[H / 64], const float (&qs)[H / 64], uint32_t scales, uint32_t offsets, float (&s)[4]) {
+    if constexpr (H == 128) {
+        asm("s_nop 7\n"  //
+            "v_mul_f32_dpp %0, %4, %6 row_newbcast:0 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %1, %4, %7 row_newbcast:1 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %2, %4, %8 row_newbcast:2 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %3, %4, %9 row_newbcast:3 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %0, %4, %10 row_newbcast:4 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %1, %4, %11 row_newbcast:5 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %2, %4, %12 row_newbcast:6 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %3, %4, %13 row_newbcast:7 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %0, %5, %14 row_newbcast:0 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %1, %5, %14 row_newbcast:1 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %2, %5, %14 row_newbcast:2 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %3, %5, %14 row_newbcast:3 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %0, %5, %15 row_newbcast:4 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %1, %5, %15 row_newbcast:5 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %2, %5, %15 row_newbcast:6 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %3, %5, %15 row_newbcast:7 row_mask:0xf bank_mask:0xf"
+            : "=&v"(s[0]), "=&v"(s[1]), "=&v"(s[2]), "=&v"(s[3])
+            : "v"(scales), "v"(offsets), "v"(acc[0][0]), "v"(acc[0][1]), "v"(acc[0][2]), "v"(acc[0][3]), "v"(acc[1][0]), "v"(acc[1][1]), "v"(acc[1][2]),
+              "v"(acc[1][3]), "v"(qs[0]), "v"(qs[1]));
+    } else {
+        asm("s_nop 7\n"
+            "v_mul_f32_dpp %0, %4, %6 row_newbcast:0 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %1, %4, %7 row_newbcast:1 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %2, %4, %8 row_newbcast:2 row_mask:0xf bank_mask:0xf\n"
+            "v_mul_f32_dpp %3, %4, %9 row_newbcast:3 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %0, %5, %10 row_newbcast:0 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %1, %5, %10 row_newbcast:1 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %2, %5, %10 row_newbcast:2 row_mask:0xf bank_mask:0xf\n"
+            "v_fmac_f32_dpp %3, %5, %10 row_newbcast:3 row_mask:0xf bank_mask:0xf"
+            : "=&v"(s[0]), "=&v"(s[1]), "=&v"(s[2]), "=&v"(s[3])
+            : "v"(scales), "v"(offsets), "v"(acc[0][0]), "v"(acc[0][1]), "v"(acc[0][2]), "v"(acc[0][3]), "v"(qs[0]));
+    }
+}
+template <int AT>  // (the lane of token 4 kq's word)
+__device__ __forceinline__ void scaled_weights(const float (&p)[4], uint32_t scales, uint32_t offsets, float (&w)[4], float& sum) {
+    asm("s_nop 3\n"
+        "v_mul_f32_dpp %0, %5, %7 row_newbcast:%c11 row_mask:0xf bank_mask:0xf\n"
+        "v_mul_f32_dpp %1, %5, %8 row_newbcast:%c12 row_mask:0xf bank_mask:0xf\n"
+        "v_mul_f32_dpp %2, %5, %9 row_newbcast:%c13 row_mask:0xf bank_mask:0xf\n"
+        "v_mul_f32_dpp %3, %5, %10 row_newbcast:%c14 row_mask:0xf bank_mask:0xf\n"
+        "v_fmac_f32_dpp %4, %6, %7 row_newbcast:%c11 row_mask:0xf bank_mask:0xf\n"
+        "v_fmac_f32_dpp %4, %6, %8 row_newbcast:%c12 row_mask:0xf bank_mask:0xf\n"
+        "v_fmac_f32_dpp %4, %6, %9 row_newbcast:%c13 row_mask:0xf bank_mask:0xf\n"
+        "v_fmac_f32_dpp %4, %6, %10 row_newbcast:%c14 row_mask:0xf bank_mask:0xf"
+        : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "+v"(sum)
+        : "v"(scales), "v"(offsets), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 1), "n"(AT + 2), "n"(AT + 3));
 }
 
 // For few rows per sequence (16 NT rows x heads of a KV head at a time).  One workgroup: one cut of the pages of a sequence, for one KV head; its four wavefronts take
 // every fourth page each, ROUND per round, and refill K as soon as the scores are done, V behind P V.
 template <int H, typename T, int NT>
-__global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4_few(AttendArgs a) {
-    constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16, G = H / 64, ROUND = 4;
+__global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4(AttendArgs a) {
+    constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16, G = H / 64, ROUND = 2;
     constexpr bool FINE = sizeof(T) == 4;
     using P4 = Page4<H>;
     __shared__ float red[4][16][LD], red_m[4][16], red_l[4][16];
@@ -103,7 +166,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4_fe
     const int m_first = rho0 / a.G, m_last = (min(rho0 + 16 * NT, R) - 1) / a.G;
     const UnitCuts uc = cuts_of(a, u, m_last);
     if (cut >= uc.n) return;
-    const int p0 = cut * uc.pages + wave, p1 = min(uc.all_pages, (cut + 1) * uc.pages);
+    const int p0 = __builtin_amdgcn_readfirstlane(cut * uc.pages + wave), p1 = __builtin_amdgcn_readfirstlane(min(uc.all_pages, (cut + 1) * uc.pages));
     const int base = a.mask ? max(a.mask_base[u.seq], 0) : 0;
     const int all_see = __builtin_amdgcn_readfirstlane(a.mask ? min(base, u.len) : min(u.ctx + m_first + 1, u.len));  // slots below are seen by every row
     Column c[NT];
@@ -133,6 +196,7 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4_fe
     const char* word_pool = reinterpret_cast<const char*>(kind ? a.vpool : a.kpool) + P4::kCodes + ((col >> 2 & (G - 1)) * 16 + kq * 4 + place) * 4;
     const char* k_pool = reinterpret_cast<const char*>(a.kpool) + lane * (ST * 4);
     const char* v_pool = reinterpret_cast<const char*>(a.vpool) + lane * (ST * 4);
+    const InRegisters bits;
     Codes4<H> x[ROUND];
     uint32_t next_word[ROUND];
     int id[ROUND], next_id[ROUND];
@@ -185,15 +249,17 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4_fe
                     acc[n][g] = floatx4{first, first, first, first};
                 }
 #pragma unroll
-            for (int st = 0; st < ST; ++st) {
-                const bf16x8 k = __builtin_bit_cast(bf16x8, code_pairs(x[j].k[st]));
+            for (int y = 0; y < ST; ++y) {  // (the groups in turn: products of one wait for each other)
+                const int st = y % G * 2 + y / G;
+                const bf16x8 k = __builtin_bit_cast(bf16x8, bits.pairs(x[j].k[st]));
 #pragma unroll
                 for (int w = 0; w < NP; ++w)
 #pragma unroll
                     for (int n = 0; n < NT; ++n) acc[n][st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[n][w][st], acc[n][st / 2], 0, 0, 0);
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n) each<4>([&](auto e) { s[j][n][e] = score_of<H, decltype(e)::value>(acc[n], qs[n], scale[j], offset[j]); });
+            for (int n = 0; n < NT; ++n) scores_of<H>(acc[n], qs[n], scale[j], offset[j], s[j][n]);
+            __builtin_amdgcn_sched_barrier(0);  // (pages one after the other: together they do not fit the registers)
         }
         if (WHOLE || i + ROUND < count) refill_k();
         if (!WHOLE || !all) {
@@ -257,36 +323,42 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4_fe
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     each<2>([&](auto b) {
-                        each<2>([&](auto half) {
-                            constexpr int B = decltype(b)::value, E = decltype(half)::value * 2, AT = word_lane<H>(1, decltype(g)::value, E);
-                            float w0 = s[j + B][n][E] * row_lane<AT>(scale[j + B]), w1 = s[j + B][n][E + 1] * row_lane<AT + 1>(scale[j + B]);
-                            float b0 = s[j + B][n][E] * row_lane<AT>(offset[j + B]), b1 = s[j + B][n][E + 1] * row_lane<AT + 1>(offset[j + B]);
-                            if constexpr (!WHOLE) {  // (a hidden token's scale may be NaN: it is not multiplied, not even by zero)
-                                const uint32_t on = ok >> ((n * ROUND + j + B) * 4 + E);
-                                w0 = on & 1 ? w0 : 0.f;
-                                b0 = on & 1 ? b0 : 0.f;
-                                w1 = on & 2 ? w1 : 0.f;
-                                b1 = on & 2 ? b1 : 0.f;
-                            }
-                            bs[n][g] += b0;
-                            bs[n][g] += b1;
-                            uint32_t pair[NW];
-                            split_pair<NW>(w0, w1, pair);
+                        constexpr int B = decltype(b)::value, AT = word_lane<H>(1, decltype(g)::value, 0);
+                        float w[4];
+                        if constexpr (WHOLE) {
+                            scaled_weights<AT>(s[j + B][n], scale[j + B], offset[j + B], w, bs[n][g]);
+                        } else {  // (a hidden token's scale may be NaN: it is not multiplied, not even by zero)
+                            each<4>([&](auto e) {
+                                constexpr int E = decltype(e)::value;
+                                const bool on = ok >> ((n * ROUND + j + B) * 4 + E) & 1u;
+                                const float p = s[j + B][n][E], ws = p * row_lane<AT + E>(scale[j + B]), wb = p * row_lane<AT + E>(offset[j + B]);
+                                w[E] = on ? ws : 0.f;
+                                bs[n][g] += on ? wb : 0.f;
+                            });
+                        }
 #pragma unroll
-                            for (int q = 0; q < NW; ++q) p[n][q][B * 2 + E / 2] = pair[q];
-                        });
+                        for (int e = 0; e < 4; e += 2) {
+                            uint32_t pair[NW];
+                            bits.split(w[e], w[e + 1], pair);
+#pragma unroll
+                            for (int q = 0; q < NW; ++q) p[n][q][B * 2 + e / 2] = pair[q];
+                        }
                     });
+                bf16x8 v[4];
                 each<4>([&](auto r) {
                     constexpr int RR = decltype(r)::value;
-                    uint4v codes = {code_pair<RR>(x[j].v[g]), code_pair<RR>(x[j].v[G + g]), code_pair<RR>(x[j + 1].v[g]), code_pair<RR>(x[j + 1].v[G + g])};
+                    uint4v codes = {bits.template pair<RR>(x[j].v[g]), bits.template pair<RR>(x[j].v[G + g]), bits.template pair<RR>(x[j + 1].v[g]), bits.template pair<RR>(x[j + 1].v[G + g])};
                     if constexpr (FINE) codes = uint4v{centred(codes[0]), centred(codes[1]), centred(codes[2]), centred(codes[3])};
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, codes);
+                    v[RR] = __builtin_bit_cast(bf16x8, codes);
+                });
 #pragma unroll
-                    for (int q = 0; q < NW; ++q)
+                for (int q = 0; q < NW; ++q)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-                            to[n][g * 4 + RR] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, p[n][q]), to[n][g * 4 + RR], 0, 0, 0);
-                });
+                            to[n][g * 4 + r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[r], __builtin_bit_cast(bf16x8, p[n][q]), to[n][g * 4 + r], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             });
         if constexpr (FINE) {
 #pragma unroll

@@ -13,21 +13,28 @@ using namespace card;
 
 namespace {
 
-// How the attention of a call is run: as over a cache of 16 bits.
-constexpr int kFewRows4 = 512;
-constexpr int kFill = 512;
-int64_t pages_uncut(int64_t groups) { return 32 + groups / 3; }
+// How the attention of a call over 4 bits is run.  R: most rows x heads of a KV head that one sequence has; all figures in us, 8 KV heads of 128.
+// Tiles of 16 rows x heads of a workgroup: one, in bf16 two for R > 1024 (R = 600 behind 3000 tokens 35 and 33, behind 14000 95 and 99; 2000 behind 300 22 and
+// 23, behind 14000 284 and 258; 8000 behind 14000 1097 and 999; 40 behind 120000 73 and 84).  Making operands of codes is work that
+// tiles share, and half as many wavefronts hide each other's waits.
+constexpr int kOneTile4 = 1024;
+// Pages are cut to have this many workgroups, three per compute unit, unless there are half of them without, counted by rows as in attend_plan (in cuts of 32, 64, 128, 256
+// pages and uncut: 64 texts of 800-8000 tokens, one row each, 97, 86, 81, 87, 135; 48 of 400-4000 39, 38, 40, 61, 61; 16 of 300-3000 17, 20, 25, 36, 36; R = 400 behind 4000
+// tokens 38, 32, 32, 38, 38; R = 600 behind 14000 126, 104, 100, 95, 163; R = 2000 behind 3000 105, 90, 84, 75, 75).
+constexpr int kFill4 = 768, kLeastCut4 = 32;
+// (one row of 3000 tokens in cuts of 16, 32 and 64 pages 10.5, 10.9, 15.3, uncut 32: a page costs 0.13 us, the join 3)
+int64_t pages_uncut4(int64_t groups) { return 40 + groups / 8; }
 AttendPlan attend4_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f32) {
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
     const int64_t most = int64_t(b->max_new > 0 ? std::min(b->max_new, b->n_rows) : b->n_rows) * G;
-    p.tiles = f32 || most <= 16 ? 1 : 2;
+    p.tiles = f32 || most <= kOneTile4 ? 1 : 2;
     p.units = int32_t(int64_t(b->n_rows) * G / (16 * p.tiles)) + b->n_seqs;
     const int pages = std::min(b->table_pages, b->max_len > 0 ? ceil_div(b->max_len, 16) : b->table_pages);
     const int full = p.units - b->n_seqs + 1;  // tiles, if the rows filled them
     const int64_t groups = int64_t(full) * cfg->n_kv_heads;
-    const bool whole = groups * 4 > kFill * 3 || pages <= pages_uncut(int64_t(std::max(full, b->n_seqs)) * cfg->n_kv_heads);
-    p.cut_pages = whole ? pages : std::max(16, ceil_div(ceil_div(groups * pages, kFill), 16) * 16);
+    const bool whole = groups * 2 > kFill4 || pages <= pages_uncut4(int64_t(std::max(full, b->n_seqs)) * cfg->n_kv_heads);
+    p.cut_pages = whole ? pages : std::max(kLeastCut4, ceil_div(ceil_div(groups * pages, kFill4), 16) * 16);
     p.cuts = ceil_div(pages, p.cut_pages);
     if (p.cuts > 1) p.bytes = size_t(p.units) * cfg->n_kv_heads * p.cuts * p.tiles * 16 * (cfg->head_dim + 2) * 4;
     return p;
@@ -45,7 +52,7 @@ void append_launch(const AppendArgs& g, int bits, int h, hipStream_t st) {
 template <int H, typename T, int NT>
 void attend4_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
     const dim3 grid(uint32_t(p.units) * uint32_t(a.Hkv), uint32_t(p.cuts));
-    hipLaunchKernelGGL((k_attend4_few<H, T, NT>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_attend4<H, T, NT>), grid, dim3(256), 0, st, a);
     if (p.cuts > 1) hipLaunchKernelGGL((k_attend_join<H, T, NT>), dim3(grid.x, 4 * NT), dim3(256), 0, st, a);
 }
 template <typename T, int NT>
@@ -66,8 +73,13 @@ int append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer,
     if (rotation) {
         g.rotate = 1;
         g.positions = rotation->positions_dev;
+        double near[8], far[8];  // powers of the base: a call takes 16 of them, not 64
+        for (int i = 0; i < 8 && !rotation->freqs_host; ++i) {
+            near[i] = std::pow(double(cfg->rope_theta), -2.0 * i / h);
+            far[i] = std::pow(double(cfg->rope_theta), -16.0 * i / h);
+        }
         for (int j = 0; j < h / 2; ++j) {
-            const double f = rotation->freqs_host ? rotation->freqs_host[j] : std::pow(double(cfg->rope_theta), -2.0 * j / h);
+            const double f = rotation->freqs_host ? rotation->freqs_host[j] : near[j % 8] * far[j / 8];
             if (!std::isfinite(f)) return CARD_EINVAL;
             g.turns[j] = f / 6.283185307179586476925;
         }

@@ -131,7 +131,7 @@ def test_scores_of_long_texts_are_compared_in_64_bits():
     x = torch.full((4, 1000), -20.0)
     for b in range(4):
         x[b, b] = 10.0
-        x[b, 100 + b] = 10.0 - 2.0 ** -8 * (b + 1)
+        x[b, 100 + b] = 10.0 - 2.0 ** -12 * (b + 1)
     scores = torch.full((1, 4), -20000.0)
     check(x, scores, 6)
     want, _ = reference(x, scores, 6)
