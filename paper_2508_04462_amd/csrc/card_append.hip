@@ -104,23 +104,27 @@ __device__ __forceinline__ void cos_sin(double turns, float& c, float& s) {
     c = at == 1 || at == 2 ? -cs : cs;
 }
 
-// Eight elements of a row of heads, as wide as they come.
-__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
-    const uint4v w = *reinterpret_cast<const uint4v*>(p);
+// Eight elements of a row of heads.
+template <typename T>
+struct Eight {
+    uint4v w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < int(sizeof(T)) / 2; ++i) w[i] = reinterpret_cast<const uint4v*>(p)[i];
     }
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const floatx4 w = reinterpret_cast<const floatx4*>(p)[i];
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __uint_as_float(w[0][i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[0][i] & 0xffff0000u);
+            }
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * i + e] = w[e];
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i / 4][i % 4]);
+        }
     }
-}
+};
 __device__ __forceinline__ uint4v packed8(const float (&x)[8]) {
     return uint4v{pack_pair(x[0], x[1]), pack_pair(x[2], x[3]), pack_pair(x[4], x[5]), pack_pair(x[6], x[7])};
 }
@@ -162,6 +166,7 @@ template <int H, typename T, int BITS>
 __global__ __launch_bounds__(256) void k_append(AppendArgs g) {
     const AttendArgs& a = g.a;
     constexpr int C = H / 16;  // pairs of 8 elements of a head
+    constexpr int U = sizeof(T) == 2 ? 4 : 2;  // of a thread, under way together
     __shared__ float2 table[16][H / 2];
     const PageRows r = rows_of_page(a, blockIdx.x);
     if (!r.some) return;
@@ -170,9 +175,9 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs g) {
     const int kt = r.t0 + tid / C, kc = tid % C;
     const bool has_k = tid < n * C;
     const T* kp = static_cast<const T*>(a.k) + (r.row0 + (has_k ? kt : r.t0)) * a.k_row + int64_t(head) * a.k_head + kc * 8;
-    float k0[8], k1[8];
-    load8(kp, k0);
-    load8(kp + H / 2, k1);
+    Eight<T> kr[2];
+    kr[0].load(kp);
+    kr[1].load(kp + H / 2);
     const T* vp = static_cast<const T*>(a.v) + int64_t(head) * a.v_head;
     constexpr int VU = BITS == 16 ? 4 * H / 256 : 1, VN = BITS == 16 ? 4 : H / 16;
     float v[VU][VN];
@@ -206,19 +211,34 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs g) {
     if (g.rotate && a.q) {
         const T* from = static_cast<const T*>(a.q) + int64_t(head) * a.G * a.q_head;
         T* to = static_cast<T*>(a.out) + int64_t(head) * a.G * a.o_head;
-        for (int e = tid; e < n * a.G * C; e += 256) {
-            const int c = e % C, at = e / C, t = r.t0 + at / a.G, q = at % a.G;
-            const T* p = from + (r.row0 + t) * a.q_row + q * a.q_head + c * 8;
-            float x0[8], x1[8];
-            load8(p, x0);
-            load8(p + H / 2, x1);
-            rotate(t, c, x0, x1);
-            T* o = to + (r.row0 + t) * a.o_row + q * a.o_head + c * 8;
-            store8(o, x0);
-            store8(o + H / 2, x1);
+        const int units = n * a.G * C;
+        for (int e0 = tid; e0 < units; e0 += 256 * U) {
+            Eight<T> x0[U], x1[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = min(e0 + u * 256, units - 1), at = e / C;
+                const T* p = from + (r.row0 + r.t0 + at / a.G) * a.q_row + at % a.G * a.q_head + e % C * 8;
+                x0[u].load(p);
+                x1[u].load(p + H / 2);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = e0 + u * 256, at = e / C, t = r.t0 + at / a.G, c = e % C;
+                if (e >= units) break;
+                float y0[8], y1[8];
+                x0[u].get(y0);
+                x1[u].get(y1);
+                rotate(t, c, y0, y1);
+                T* o = to + (r.row0 + t) * a.o_row + at % a.G * a.o_head + c * 8;
+                store8(o, y0);
+                store8(o + H / 2, y1);
+            }
         }
     }
     if (r.stored == 0) return;
+    float k0[8], k1[8];
+    kr[0].get(k0);
+    kr[1].get(k1);
     if (g.rotate && has_k) rotate(kt, kc, k0, k1);
     if constexpr (BITS == 16) {
         const size_t base = (size_t(r.page) * a.Hkv + head) * (16 * H);

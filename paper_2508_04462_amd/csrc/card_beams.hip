@@ -10,6 +10,7 @@
 namespace card {
 
 constexpr int kMostBeams = 32;
+constexpr int kHistoryLoads = 4;  // of a thread, under way together
 
 struct BeamArgs {
     LogprobArgs rows;  // (top: beams to go on with)
@@ -32,12 +33,29 @@ __global__ __launch_bounds__(kLpThreads) void k_beam_rows(BeamArgs b) {
     __shared__ LogprobShared sm;
     const int row = blockIdx.x, part = blockIdx.y;
     if (b.done && b.done[row] != 0) return;
-    const RowSums r = scan_part<T>(b.rows, sm, row, part);
+    const RowSums r = scan_part<T, false>(b.rows, sm, row, part);
     leave_part(b.rows, sm, r, row, part);
 }
 
-// One workgroup: one group.  A wavefront puts the parts of a beam together; then a candidate's place is the number of better ones.  Candidates with equal scores
-// go by beam, then by token; a beam's list has them in that order.
+// Scores as numbers in the same order; 0: none.
+__device__ __forceinline__ unsigned long long score_key(double s) {
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, s);
+    return s > -INFINITY ? (u >> 63 ? ~u : u | 1ull << 63) : 0ull;
+}
+__device__ __forceinline__ unsigned long long max_of_lanes(unsigned long long v) {
+    v = group_max<16>(v);
+    unsigned long long most = lane_key(v, 0);
+#pragma unroll
+    for (int row = 16; row < 64; row += 16) {
+        const unsigned long long other = lane_key(v, row);
+        most = other > most ? other : most;
+    }
+    return most;
+}
+
+// One workgroup: one group, or where histories are long a share of its new beams, which are chosen again by each.  A wavefront puts the parts of a beam together; then one
+// wavefront, a beam a lane, takes the best of the lists' heads as often as there are beams to go on with, or ranks short lists at once.  Candidates with equal scores go by beam, then by token; a beam's list
+// has them in that order.
 __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
     __shared__ double score[kMostBeams * kMaxTop];
     __shared__ int token[kMostBeams * kMaxTop];
@@ -65,8 +83,19 @@ __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
             r = join_lanes(r, c);
             TopList list;
             const unsigned long long* keys = a.part_keys + size_t(row) * n;
-            if (a.parts >= top) list.floor(lane < a.parts ? uint32_t(keys[lane * top] >> 32) : 0u, top);  // of the parts' first keys, the top-th largest
-            for (int i = 0; i < n; i += 64) list.offer(i + lane < n ? keys[i + lane] : 0ull, top, lane);
+            if (n <= 64) {
+                const unsigned long long key = lane < n ? keys[lane] : 0ull;
+                if (a.parts > 3) list.floor(uint32_t(key >> 32), top);
+                list.offer(key, top, lane);
+            } else {  // rank by rank over the parts, whose lists are in order: where none of a rank enters, none behind it does
+                for (int i = 0; i < n; i += 64) {
+                    const uint32_t at = uint32_t(i + lane), parts = uint32_t(a.parts);
+                    const unsigned long long key = at < uint32_t(n) ? keys[at % parts * top + at / parts] : 0ull;
+                    if (i == 0) list.floor(uint32_t(key >> 32), top);
+                    if (i > 0 && a.parts <= 64 && !__ballot(key > list.least)) break;
+                    list.offer(key, top, lane);
+                }
+            }
             // (a NaN or +inf among the logits has made s NaN: no candidates)
             if (lane < top && list.best != 0ull && r.s > 0.f) {
                 mine = held + ((double(key_logit(list.best)) - double(r.m)) / b.temperature - log(double(r.s)));
@@ -80,24 +109,42 @@ __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
     }
     if (tid < top) parent_of[tid] = -1;
     __syncthreads();
-    const int all = b.beams * top;
-    for (int i = tid; i < all; i += blockDim.x) {
-        const double s = score[i];
-        if (!(s > -INFINITY)) continue;
-        int better = 0;
-        for (int j = 0; j < all; ++j) better += score[j] > s || (score[j] == s && j < i);
-        if (better >= top) continue;
+    const auto take = [&](int k, int i) {  // entry i of the lists is new beam k
         const int beam = i / top;
-        const size_t to = size_t(group) * top + better;
-        parent_of[better] = beam;
-        token_of[better] = token[i];
-        b.out_scores[to] = float(s);
+        parent_of[k] = beam;
+        token_of[k] = token[i];
+        if (blockIdx.y > 0) return;
+        const size_t to = size_t(group) * top + k;
+        b.out_scores[to] = float(score[i]);
         b.out_tokens[to] = token[i];
         b.out_parents[to] = beam;
         if (b.out_done) b.out_done[to] = (b.done && b.done[group * b.beams + beam] != 0) || (b.eos >= 0 && token[i] == b.eos);
+    };
+    const int all = b.beams * top;
+    if (wave == 0 && all <= 64) {  // a lane each: its place is the number of better ones (a search of 4 beams 6.0 us, taken one by one 7.8)
+        const unsigned long long mine = lane < all ? score_key(score[lane]) : 0ull;
+        int better = 0;
+        for (int j = 0; j < all; ++j) {
+            const unsigned long long other = lane_key(mine, j);
+            better += other > mine || (other == mine && j < lane);
+        }
+        if (mine != 0ull && better < top) take(better, lane);
+    } else if (wave == 0) {
+        int at = lane * top, left = lane < b.beams ? top : 0;
+        unsigned long long head = left > 0 ? score_key(score[at]) : 0ull, next = left > 1 ? score_key(score[at + 1]) : 0ull;
+        for (int k = 0; k < top; ++k) {
+            const unsigned long long best = max_of_lanes(head);
+            if (best == 0ull) break;
+            if (lane != __ffsll(__ballot(head == best)) - 1) continue;
+            take(k, at);
+            head = next;
+            ++at;
+            --left;
+            next = left > 1 ? score_key(score[at + 1]) : 0ull;
+        }
     }
     __syncthreads();
-    if (tid < top && parent_of[tid] < 0) {  // fewer candidates than that
+    if (blockIdx.y == 0 && tid < top && parent_of[tid] < 0) {  // fewer candidates than that
         const size_t to = size_t(group) * top + tid;
         b.out_scores[to] = -INFINITY;
         b.out_tokens[to] = -1;
@@ -106,11 +153,18 @@ __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
     }
     if (!b.history) return;
     const int len = min(max(b.lengths[group], 0), b.history_len);
-    for (int k = 0; k < top; ++k) {
+    for (int k = blockIdx.y; k < top; k += gridDim.y) {
         if (parent_of[k] < 0) continue;
         const int32_t* from = b.history + (size_t(group) * b.beams + parent_of[k]) * b.history_len;
         int32_t* to = b.out_history + (size_t(group) * top + k) * b.history_len;
-        for (int i = tid; i < len; i += blockDim.x) to[i] = from[i];
+        for (int i = tid; i < len; i += blockDim.x * kHistoryLoads) {
+            int32_t v[kHistoryLoads];
+#pragma unroll
+            for (int u = 0; u < kHistoryLoads; ++u) v[u] = from[min(i + u * int(blockDim.x), len - 1)];
+#pragma unroll
+            for (int u = 0; u < kHistoryLoads; ++u)
+                if (i + u * int(blockDim.x) < len) to[i + u * blockDim.x] = v[u];
+        }
         if (tid == 0 && len < b.history_len) to[len] = token_of[k];
     }
 }

@@ -56,10 +56,11 @@ struct RowSums {
         s *= e;
         m = mnew;
     }
+    template <bool ENTROPY>
     __device__ __forceinline__ void add(float x, float c) {
         const float d = (x - m) * c, e = __builtin_amdgcn_exp2f(d);
         s += e;
-        t = fmaf(e, fmaxf(d, -1e4f), t);
+        if constexpr (ENTROPY) t = fmaf(e, fmaxf(d, -1e4f), t);
     }
     __device__ __forceinline__ void join(RowSums b, float c) {
         const float mnew = fmaxf(m, b.m);
@@ -186,7 +187,8 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, const LogprobSh
 
 // A workgroup's part of a row, in turns of kLpVecs 16-byte loads a lane: returns its sums, and leaves its most probable tokens in sm.out.  The loads are of aligned units, whatever the row begins at:
 // what a unit holds before the row or behind it is not read.
-template <typename T>
+// ENTROPY: with t, which costs two instructions a logit.
+template <typename T, bool ENTROPY>
 __device__ __forceinline__ RowSums scan_part(const LogprobArgs& a, LogprobShared& sm, int row, int part) {
     constexpr int VN = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 63;
@@ -234,7 +236,7 @@ __device__ __forceinline__ RowSums scan_part(const LogprobArgs& a, LogprobShared
 #pragma unroll
         for (int u = 0; u < kLpVecs; ++u)
 #pragma unroll
-            for (int e = 0; e < VN; ++e) turn.add(x[u][e], c);
+            for (int e = 0; e < VN; ++e) turn.add<ENTROPY>(x[u][e], c);
         r.s += turn.s;
         r.t += turn.t;
         if (a.top == 0) continue;
@@ -272,7 +274,7 @@ template <typename T>
 __global__ __launch_bounds__(kLpThreads) void k_logprobs(LogprobArgs a) {
     __shared__ LogprobShared sm;
     const int row = blockIdx.x, part = blockIdx.y;
-    const RowSums r = scan_part<T>(a, sm, row, part);
+    const RowSums r = scan_part<T, true>(a, sm, row, part);
     if (a.parts == 1) finish_row<T>(a, sm, r, row);
     else leave_part(a, sm, r, row, part);
 }

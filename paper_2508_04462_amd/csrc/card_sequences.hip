@@ -60,6 +60,8 @@ void attend4_launch(const AttendArgs& a, const AttendPlan& p, int h, hipStream_t
     h == 128 ? attend4_launch<128, T, NT>(a, p, st) : attend4_launch<64, T, NT>(a, p, st);
 }
 
+constexpr int kHistoryShare = 1024;  // of a workgroup of k_beam_join (tokens)
+
 int append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_t layer, int bits, const card_rotation* rotation, const card_rows* q,
            const card_rows* q_out, const card_rows* k, const card_rows* v, void* stream) {
     if (const int st = layer_refused(cfg, batch, layer)) return st;
@@ -174,7 +176,7 @@ int card_beam_select(const void* logits_dev, int32_t type, int32_t vocab, int64_
     a.part_vecs = ceil_div(units, parts);
     a.parts = ceil_div(units, a.part_vecs);
     a.part_sums = static_cast<float*>(workspace_dev);
-    a.part_keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace_dev) + logprob_sums_bytes(rows, vocab));
+    a.part_keys = reinterpret_cast<unsigned long long*>(static_cast<char*>(workspace_dev) + size_t(rows) * parts * 16);
     b.beams = beams->beams;
     b.eos = beams->eos_token;
     b.history_len = beams->history_len;
@@ -192,7 +194,9 @@ int card_beam_select(const void* logits_dev, int32_t type, int32_t vocab, int64_
     hipStream_t st = as_stream(stream);
     if (type == CARD_F32) hipLaunchKernelGGL(k_beam_rows<float>, grid, dim3(kLpThreads), 0, st, b);
     else hipLaunchKernelGGL(k_beam_rows<__bf16>, grid, dim3(kLpThreads), 0, st, b);
-    hipLaunchKernelGGL(k_beam_join, dim3(uint32_t(beams->groups)), dim3(64 * uint32_t(std::min(std::max(beams->beams, 4), 16))), 0, st, b);
+    const int64_t moved = b.history ? int64_t(b.history_len) * a.top : 0;
+    const uint32_t shares = uint32_t(std::max(int64_t(1), std::min(int64_t(a.top), moved / kHistoryShare)));
+    hipLaunchKernelGGL(k_beam_join, dim3(uint32_t(beams->groups), shares), dim3(64 * uint32_t(std::min(std::max(beams->beams, 4), 16))), 0, st, b);
     return launch_status();
 }
 
