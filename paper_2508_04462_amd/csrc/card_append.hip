@@ -161,7 +161,9 @@ __device__ __forceinline__ PageRows rows_of_page(const AttendArgs& a, int unit) 
 
 // One workgroup: the rows of one page of a sequence, for one KV head and the query heads that share it.  Angles are the same for all heads: each is
 // made once, into LDS, while the rows are on their way.  A thread rotates elements 8 c .. + 7 with their partners half a head further on; products are added in 64 bits,
-// which makes a rotated value the exact one's rounding, the same wherever it is computed, and costs less than reading it.
+// which makes a rotated value the exact one's rounding, the same wherever it is computed, and costs less than reading it.  Bound by memory for prompts (2000
+// rows of 64 + 8 heads of 128, 82 MB, in 16 us, 5.1 TB/s; a row of queries at a time 18.5; keys and queries in workgroups of their own 18.6), by latency for few rows (5.0 us). To 4 bits, about
+// 2280 rows of 28 + 4 heads, 13 us.
 template <int H, typename T, int BITS>
 __global__ __launch_bounds__(256) void k_append(AppendArgs g) {
     const AttendArgs& a = g.a;

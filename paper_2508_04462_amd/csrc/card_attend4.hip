@@ -72,8 +72,8 @@ __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>)
 template <int N, typename F>
 __device__ __forceinline__ void each(F&& f) { each_of<N>(f, std::make_integer_sequence<int, N>{}); }
 
-// With fp32 rows sums keep to small numbers: scores begin at -24 sum q, which makes theirs sums of (c - 8) q, values enter as c - 8, with the offset of code 8 in place of b,
-// and each round's products with values are added up on their own.  (Otherwise o and sum p b are some 24 scales each and nearly cancel.)
+// With fp32 rows sums keep to small numbers: codes enter as c - 8, with the offset of code 8 in place of b, and each round's products with values are added up on their
+// own.  (Otherwise a sum of products and its offsets are some 24 scales each, and nearly cancel.)
 constexpr float kMiddle = 24.f;
 
 // Sums of a row's query over the channels of each group, of the parts that the products take.
@@ -149,8 +149,13 @@ __device__ __forceinline__ void scaled_weights(const float (&p)[4], uint32_t sca
         : "v"(scales), "v"(offsets), "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(AT), "n"(AT + 1), "n"(AT + 2), "n"(AT + 3));
 }
 
-// For few rows per sequence (16 NT rows x heads of a KV head at a time).  One workgroup: one cut of the pages of a sequence, for one KV head; its four wavefronts take
-// every fourth page each, ROUND per round, and refill K as soon as the scores are done, V behind P V.
+// 16 NT rows x heads of a KV head at a time.  One workgroup: one cut of the pages of a sequence, for one KV head; its four wavefronts take every fourth page each, two per
+// round, and refill K as soon as the scores are done, V behind P V.  Bound by vector instructions: a round of two pages is 278 of them (558 as the compiler makes them
+// of the same formulas, see InRegisters and scores_of), 128 to make operands of codes, which two tiles share, and some 150 a tile; and 24 matrix instructions a tile.  64 texts of 800-8000
+// tokens, a row of 4 heads each, 334 MB, in 84 us (4.0 TB/s; vector units busy 63 % of the time with twice the instructions, in 101); 5 rows x 8 behind 120000 tokens 69;
+// 2000 rows x 4 behind 14000 1000, 0.49 PFLOP/s, with the second part of the weights 0.74.  Four pages per round with two wavefronts per SIMD 105 for the 64 texts,
+// with three, spilling, 148.  A kernel for many rows whose wavefronts share pages made operands in LDS (two tiles a wavefront, four wavefronts) took 950 for the
+// 2000 rows, but 44 for 500 rows behind 300 tokens against 22 and 257 for three texts of up to 1000 rows x 7 against 229.
 template <int H, typename T, int NT>
 __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4(AttendArgs a) {
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16, G = H / 64, ROUND = 2;
@@ -244,14 +249,13 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4(At
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const float first = FINE ? -kMiddle * qs[n][g] : 0.f;
-                    acc[n][g] = floatx4{first, first, first, first};
-                }
+                for (int g = 0; g < G; ++g) acc[n][g] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int y = 0; y < ST; ++y) {  // (the groups in turn: products of one wait for each other)
                 const int st = y % G * 2 + y / G;
-                const bf16x8 k = __builtin_bit_cast(bf16x8, bits.pairs(x[j].k[st]));
+                uint4v codes = bits.pairs(x[j].k[st]);
+                if constexpr (FINE) codes = uint4v{centred(codes[0]), centred(codes[1]), centred(codes[2]), centred(codes[3])};
+                const bf16x8 k = __builtin_bit_cast(bf16x8, codes);
 #pragma unroll
                 for (int w = 0; w < NP; ++w)
 #pragma unroll

@@ -129,45 +129,51 @@ __global__ __launch_bounds__(H / 64 * 192) void k_kv_move_slots(MoveArgs a) {
         });
 }
 
-// The same in pages of 4 bits a value (Page4).  One workgroup: one head of one layer, a wavefront for K and one for V; a lane owns a piece of a token for all moves (K: a word, V: the
-// two bytes of four channels, and the words behind the codes), and all of a round is read before any is written, which is the order of the list, as above.  1500 tokens of 32
-// layers x 8 heads x 128: MOVED.
-constexpr int kMoveRound4 = 32;  // loads of a lane
+// The same in pages of 4 bits a value (Page4).  One workgroup: one head of one layer, a wavefront for K and one for V; sixteen lanes have a token, a lane the words or bytes of its
+// channels for all moves, and all of a round is read before any is written, which is the order of the list, as above.  1500 tokens of 32 layers x 8 heads x 128 152 us (a token after the other
+// 700), 128 13, 32 6.5.  157 pages are copied by k_kv_copy_pages in 23 us.
+constexpr int kMoveRound4 = 24;  // tokens of a lane: four times as many in a round
 template <int H>
 __global__ __launch_bounds__(128) void k_kv4_move_slots(MoveArgs a) {
     using P = Page4<H>;
     constexpr int G = H / 64, R = kMoveRound4;
-    const int head = blockIdx.x, lane = threadIdx.x & 63, first = blockIdx.z * a.part, end = min(a.n, first + a.part);
+    __shared__ int src[kMoveSlots], dst[kMoveSlots];
+    const int head = blockIdx.x, lane = threadIdx.x & 63, at = lane & 15, sub = lane >> 4, first = blockIdx.z * a.part, n = min(a.n, first + a.part) - first;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const auto rounds = [&](auto per, int sub, bool owns, auto&& read, auto&& write) {  // per: moves of a load
-        constexpr int PER = decltype(per)::value;
-        for (int i = first; i < end; i += R * PER) {
-            uint32_t v[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) v[r] = read(a.src[min(i + r * PER + sub, end - 1)]);
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (owns && i + r * PER + sub < end) write(a.dst[i + r * PER + sub], v[r]);
-        }
-    };
-    char* pool = reinterpret_cast<char*>((wave == 0 ? a.kpool : a.vpool) + blockIdx.y * a.layer_elems);
-    const auto page_at = [&](int slot) { return pool + P::at(slot >> 4, a.n_kv_heads, head); };
-    if (wave == 0) {
-        constexpr int SLOTS = H / 4;
-        const int piece = min(lane % SLOTS, H / 8 + G - 1);
-        const auto word = [&](int slot) { return reinterpret_cast<uint32_t*>(page_at(slot)) + (piece < H / 8 ? P::k_word(piece, slot & 15) : P::word(piece - H / 8, slot & 15)); };
-        rounds(std::integral_constant<int, 64 / SLOTS>{}, lane / SLOTS, lane % SLOTS < H / 8 + G, [&](int slot) { return *word(slot); }, [&](int slot, uint32_t v) { *word(slot) = v; });
-        return;
+    for (int i = threadIdx.x; i < n; i += 128) {
+        src[i] = a.src[first + i];
+        dst[i] = a.dst[first + i];
     }
-    constexpr int SLOTS = H / 2;
-    const int piece = min(lane % SLOTS, 17 * G - 1);
-    const auto half = [&](int slot) { return reinterpret_cast<unsigned short*>(page_at(slot)) + P::v_half(piece & 15, piece >> 4, slot & 15); };
-    const auto word = [&](int slot) { return reinterpret_cast<uint32_t*>(page_at(slot)) + P::word(piece - 16 * G, slot & 15); };
-    rounds(std::integral_constant<int, 64 / SLOTS>{}, lane / SLOTS, lane % SLOTS < 17 * G, [&](int slot) { return piece < 16 * G ? uint32_t(*half(slot)) : *word(slot); },
-           [&](int slot, uint32_t v) {
-               if (piece < 16 * G) *half(slot) = static_cast<unsigned short>(v);
-               else *word(slot) = v;
-           });
+    __syncthreads();
+    char* pool = reinterpret_cast<char*>((wave == 0 ? a.kpool : a.vpool) + blockIdx.y * a.layer_elems);
+    const auto words = [&](int slot) { return reinterpret_cast<uint32_t*>(pool + P::at(slot >> 4, a.n_kv_heads, head)); };
+    const auto halves = [&](int slot) { return reinterpret_cast<unsigned short*>(words(slot)); };
+    for (int i = sub; i < n + sub; i += 4 * R) {
+        uint32_t code[R][G], word[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int slot = src[min(i + 4 * r, n - 1)], t = slot & 15;
+            if (wave > 0) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) code[r][g] = halves(slot)[P::v_half(at, g, t)];
+            } else if (at < H / 8) {
+                code[r][0] = words(slot)[P::k_word(at, t)];
+            }
+            if (at < G) word[r] = words(slot)[P::word(at, t)];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (i + 4 * r >= n) continue;
+            const int slot = dst[i + 4 * r], t = slot & 15;
+            if (wave > 0) {
+#pragma unroll
+                for (int g = 0; g < G; ++g) halves(slot)[P::v_half(at, g, t)] = static_cast<unsigned short>(code[r][g]);
+            } else if (at < H / 8) {
+                words(slot)[P::k_word(at, t)] = code[r][0];
+            }
+            if (at < G) words(slot)[P::word(at, t)] = word[r];
+        }
+    }
 }
 
 }  // namespace card

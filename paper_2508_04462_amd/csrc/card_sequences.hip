@@ -22,8 +22,8 @@ constexpr int kOneTile4 = 1024;
 // pages and uncut: 64 texts of 800-8000 tokens, one row each, 97, 86, 81, 87, 135; 48 of 400-4000 39, 38, 40, 61, 61; 16 of 300-3000 17, 20, 25, 36, 36; R = 400 behind 4000
 // tokens 38, 32, 32, 38, 38; R = 600 behind 14000 126, 104, 100, 95, 163; R = 2000 behind 3000 105, 90, 84, 75, 75).
 constexpr int kFill4 = 768, kLeastCut4 = 32;
-// (one row of 3000 tokens in cuts of 16, 32 and 64 pages 10.5, 10.9, 15.3, uncut 32: a page costs 0.13 us, the join 3)
-int64_t pages_uncut4(int64_t groups) { return 40 + groups / 8; }
+// (uncut and in cuts of 32: one row of 1000 tokens 11.7 and 11.8, of 1500 15.7 and 12.0, of 3000 32 and 11; R = 400 behind 1000 13.0 and 15.8, in fp32 behind 1024 14.3 and 15.2)
+int64_t pages_uncut4(int64_t groups) { return 64 + groups / 8; }
 AttendPlan attend4_plan(const card_model_cfg* cfg, const card_kv_batch* b, bool f32) {
     AttendPlan p = {};
     const int G = cfg->n_q_heads / cfg->n_kv_heads;

@@ -357,6 +357,58 @@ class Target:
         res = {"logprob": logprob[:n - 1], "entropy": entropy}
         return dict(res, top_tokens=top_tokens, top_logprobs=top_logprobs) if top > 0 else res
 
+    def beam_search(self, pool, tokens: Sequence[int], beams: int, n_tokens: int, eos: int = -1, temperature: float = 1.0) -> Dict:
+        """The `beams` texts behind a prompt that a beam search of n_tokens steps finds: "tokens", a list of each (its last token eos where it has
+        ended), and "scores", sums of ln softmax(logits / temperature), best first.  The beams are sequences of `pool` (a SequencePool of the Target's
+        layers and heads), which share the prompt's pages and those of common beginnings; an ended one is not forwarded any more.  CARD_ECAPACITY where the pool or max_ctx has
+        no room; the sequences are freed at the end, and the Target is on what it was attached to."""
+        from .sequences import beam_select
+
+        n = len(tokens)
+        if n < 1 or beams < 1 or n_tokens < 1 or min(tokens) < 0 or max(tokens) >= self.cfg.vocab:
+            raise B.CardError(B.CARD_ERANGE, "beam_search")
+        before, dev = self._attached, self.device
+        seqs = [pool.new()]
+        failed = torch.zeros((), dtype=torch.int32, device=dev)
+        logits = torch.empty((beams, self.cfg.vocab), dtype=torch.float32, device=dev)
+        scores = torch.zeros((1, 1), dtype=torch.float32, device=dev)
+        lengths = torch.zeros(1, dtype=torch.int32, device=dev)
+        cand = torch.tensor([int(tokens[-1])], dtype=torch.int32, device=dev)
+        done, history = None, torch.zeros((1, 1, n_tokens), dtype=torch.int32, device=dev)
+        ended = [0]
+        try:
+            pool.extend(seqs[0], n)
+            self.attach(pool, seqs[0])
+            if n > 1:
+                self.prefill(tokens[:-1])
+                failed = torch.minimum(failed, self.out[0])
+            for step in range(n_tokens):
+                for i, seq in enumerate(seqs):
+                    if not ended[i]:
+                        self.attach(pool, seq)
+                        _check(self.enqueue_verify(n - 1 + step, -1, 1, logits[i:i + 1], cand=cand[i:i + 1]), "card_verify")
+                        failed = torch.minimum(failed, self.out[0])
+                got = beam_select(logits[:len(seqs)], scores, beams, done, eos, temperature, history, lengths)
+                scores, done, history, cand = got["scores"], got["done"], got["history"], got["tokens"][0]
+                lengths = lengths + 1
+                *said, status = torch.cat([got["parents"][0], done[0], failed.view(1)]).tolist()
+                if status < 0:  # weights not packed
+                    raise B.CardError(B.CARD_EDEVICE, "beam_search")
+                ended = said[beams:]
+                seqs = pool.reorder(seqs, said[:beams])
+                if all(ended) or step + 1 == n_tokens:
+                    break
+                for i, seq in enumerate(seqs):
+                    if not ended[i]:
+                        pool.extend(seq, 1)
+        finally:
+            self._attached = before
+            for seq in seqs:
+                pool.free(seq)
+        texts, found = history[0, :, :step + 1].tolist(), scores[0].tolist()
+        cut = [t.index(eos) + 1 if eos in t else len(t) for t in texts]
+        return {"tokens": [t[:c] for t, c, s in zip(texts, cut, found) if s > float("-inf")], "scores": [s for s in found if s > float("-inf")]}
+
     def release_prompt_workspace(self) -> None:
         """Give the memory back that prompts work in (8B shape: 0.25 GB; the next prompt takes it again)."""
         self._prompt_ws, self._prompt_rows = None, 0

@@ -263,16 +263,22 @@ class SequencePool:
             _check(call(cfg, plan.batch, layer, B.card_rotation(freqs, positions), *rows, self._stream()), "card_kv_append")
         return out
 
-    def read(self, plan: AttendPlan, layer: int, dtype: torch.dtype = torch.float32):
-        """card_kv4_read: keys and values [rows][kv heads][h] of the plan's rows as a pool of 4 bits holds them."""
+    def read(self, seq: int, layer: int, first: int = 0, end: Optional[int] = None, dtype: torch.dtype = torch.float32):
+        """card_kv4_read: keys and values [end - first][kv heads][h] of tokens first .. end - 1 of a sequence (to its end), as a pool of 4 bits holds them."""
         if self.bits != 4:
             raise ValueError("of pools of 4 bits (else card_kv_gather)")
-        cfg = self.cfg
-        k, v = (torch.empty((plan.n_rows, cfg.n_kv_heads, cfg.head_dim), dtype=dtype, device=self.device) for _ in range(2))
-        if plan.n_rows > 0:
-            self._still_holds(plan, False, "read")
+        s, cfg = self._seqs[seq], self.cfg
+        end = s.length if end is None else end
+        if not 0 <= first <= end <= s.length:
+            raise B.CardError(B.CARD_ERANGE, "read")
+        n = end - first
+        k, v = (torch.empty((n, cfg.n_kv_heads, cfg.head_dim), dtype=dtype, device=self.device) for _ in range(2))
+        if n > 0:
+            at = torch.tensor([first, 0, n], dtype=torch.int32, device=self.device)
+            batch = B.CardKVBatch(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.n_pages, 1, s.table.data_ptr(), s.table.numel(), n, at.data_ptr(),
+                                  at.data_ptr() + 4, n, end)
             with torch.cuda.device_of(self.k_pages):
-                _check(B.card_kv4_read(cfg, plan.batch, layer, B.card_rows(k), B.card_rows(v), self._stream()), "card_kv4_read")
+                _check(B.card_kv4_read(cfg, batch, layer, B.card_rows(k), B.card_rows(v), self._stream()), "card_kv4_read")
         return k, v
 
     def _look_at_rows(self, plan: AttendPlan, *rows) -> None:
