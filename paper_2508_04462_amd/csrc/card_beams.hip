@@ -38,6 +38,7 @@ __global__ __launch_bounds__(kLpThreads) void k_beam_rows(BeamArgs b) {
     leave_part(b.rows, sm, r, row, part);
 }
 
+__device__ __forceinline__ float first_lane(float v) { return __uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(v))))); }
 // Scores as numbers in the same order; 0: none.
 __device__ __forceinline__ unsigned long long score_key(double s) {
     const unsigned long long u = __builtin_bit_cast(unsigned long long, s);
@@ -82,6 +83,8 @@ __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
                 r.join(RowSums{v[0], v[1], v[2]}, c);
             }
             r = join_lanes(r, c);
+            // (one lane's, for all: each adds up in another order, and equal logits are to have equal scores)
+            const float most = first_lane(r.m), total = first_lane(r.s);
             TopList list;
             const unsigned long long* keys = a.part_keys + size_t(row) * n;
             if (n <= 64) {
@@ -98,8 +101,8 @@ __global__ __launch_bounds__(1024) void k_beam_join(BeamArgs b) {
                 }
             }
             // (a NaN or +inf among the logits has made s NaN: no candidates)
-            if (lane < top && list.best != 0ull && r.s > 0.f) {
-                mine = held + ((double(key_logit(list.best)) - double(r.m)) / b.temperature - log(double(r.s)));
+            if (lane < top && list.best != 0ull && total > 0.f) {
+                mine = held + ((double(key_logit(list.best)) - double(most)) / b.temperature - log(double(total)));
                 tok = int(0xffffffffu - uint32_t(list.best));
             }
         }

@@ -126,6 +126,25 @@ def test_equal_scores():
     assert got["parents"][0].tolist() == [0, 1] and got["tokens"][0].tolist() == [200, 4]
 
 
+def test_equal_logits_of_a_row():
+    """Logits in coarse steps, so that the best of a row are equal by twos and more, in rows of several parts whose sums are any numbers."""
+    for seed in range(6):
+        g = torch.Generator().manual_seed(seed)
+        for groups, beams, vocab in ((1, 1, 30011), (20, 6, 20011), (60, 5, 9001)):
+            x = (torch.randn((groups * beams, vocab), generator=g) * 3).round() * 0.25
+            x[:, ::7] += torch.rand((groups * beams, 1), generator=g).bfloat16().float() * 0.125
+            scores = -torch.rand((groups, beams), generator=g) * 20 - 600
+            want, _ = reference(x.bfloat16(), scores, beams + 2)
+            import paper_2508_04462_amd as card
+
+            got = card.beam_select(x.bfloat16().cuda(), scores.cuda(), beams + 2)
+            for a in range(groups):  # (of different beams, candidates may be as near as their scores are certain)
+                far = all(p == q or abs(s - t) > 4e-6 for p, q, s, t in zip(want["parents"][a], want["parents"][a][1:], want["scores"][a], want["scores"][a][1:]))
+                if far:
+                    assert torch.equal(got["parents"][a].cpu().long(), want["parents"][a]), (seed, groups, a)
+                    assert torch.equal(got["tokens"][a].cpu().long(), want["tokens"][a]), (seed, groups, a)
+
+
 def test_scores_of_long_texts_are_compared_in_64_bits():
     """Sums of thousands, between which fp32 has no room for the candidates' differences."""
     x = torch.full((4, 1000), -20.0)
