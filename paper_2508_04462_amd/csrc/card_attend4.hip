@@ -152,7 +152,7 @@ __device__ __forceinline__ void scaled_weights(const float (&p)[4], uint32_t sca
 // 16 NT rows x heads of a KV head at a time.  One workgroup: one cut of the pages of a sequence, for one KV head; its four wavefronts take every fourth page each, two per
 // round, and refill K as soon as the scores are done, V behind P V.  Bound by vector instructions: a round of two pages is 278 of them (558 as the compiler makes them
 // of the same formulas, see InRegisters and scores_of), 128 to make operands of codes, which two tiles share, and some 150 a tile; and 24 matrix instructions a tile.  64 texts of 800-8000
-// tokens, a row of 4 heads each, 334 MB, in 84 us (4.0 TB/s; vector units busy 63 % of the time with twice the instructions, in 101); 5 rows x 8 behind 120000 tokens 69;
+// tokens, a row of 4 heads each, 334 MB, in 84 us (4.0 TB/s; vector units busy 56 % of the time, matrix units 14; loads alone 70); 5 rows x 8 behind 120000 tokens 69;
 // 2000 rows x 4 behind 14000 1000, 0.49 PFLOP/s, with the second part of the weights 0.74.  Four pages per round with two wavefronts per SIMD 105 for the 64 texts,
 // with three, spilling, 148.  A kernel for many rows whose wavefronts share pages made operands in LDS (two tiles a wavefront, four wavefronts) took 950 for the
 // 2000 rows, but 44 for 500 rows behind 300 tokens against 22 and 257 for three texts of up to 1000 rows x 7 against 229.
