@@ -76,7 +76,7 @@ class CardRowMask(C.Structure):
 
 class CardRotation(C.Structure):
     _fields_ = [("freqs_host", C.c_void_p), ("positions_dev", C.c_void_p)]
-    head_dim = 0  # that the frequencies are for (0: no frequencies, or not said)
+    head_dim = None  # that the frequencies are for (None: no frequencies, or not said)
 
 
 class CardBeams(C.Structure):
@@ -459,14 +459,14 @@ def card_rotation(freqs=None, positions=None) -> CardRotation:
     keeps the frequencies; the positions are the caller's to keep."""
     table = None if freqs is None else (C.c_double * len(freqs))(*[float(f) for f in freqs])
     rotation = CardRotation(None if table is None else C.addressof(table), _ptr(positions))
-    rotation.table, rotation.head_dim = table, 0 if freqs is None else 2 * len(freqs)
+    rotation.table, rotation.head_dim = table, None if freqs is None else 2 * len(freqs)
     return rotation
 
 
 def card_kv_append(cfg, batch: CardKVBatch, layer: int, rotation: Optional[CardRotation], q: Optional[CardRows], q_out: Optional[CardRows],
                    k: CardRows, v: CardRows, stream=None) -> int:
     """rotation: what card_rotation gives, or None."""
-    if rotation is not None and rotation.head_dim and rotation.head_dim != cfg.head_dim:
+    if rotation is not None and rotation.head_dim not in (None, cfg.head_dim):
         return CARD_EINVAL
     return lib.card_kv_append(cfg, batch, layer, rotation, q, q_out, k, v, _ptr(stream))
 
@@ -477,7 +477,7 @@ def card_kv4_pool_bytes(cfg, n_pages: int) -> int:
 
 def card_kv4_append(cfg, batch: CardKVBatch, layer: int, rotation: Optional[CardRotation], q: Optional[CardRows], q_out: Optional[CardRows],
                     k: CardRows, v: CardRows, stream=None) -> int:
-    if rotation is not None and rotation.head_dim and rotation.head_dim != cfg.head_dim:
+    if rotation is not None and rotation.head_dim not in (None, cfg.head_dim):
         return CARD_EINVAL
     return lib.card_kv4_append(cfg, batch, layer, rotation, q, q_out, k, v, _ptr(stream))
 

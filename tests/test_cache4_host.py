@@ -46,6 +46,7 @@ def test_append_refusals(name):
     for bad in (math.nan, math.inf, -math.inf):
         assert call(rotation=card.card_rotation([bad] + model_freqs(1e4, 64)[1:])) == card.CARD_EINVAL
     assert call(rotation=card.card_rotation(model_freqs(1e4, 128))) == card.CARD_EINVAL  # of another head size
+    assert call(rotation=card.card_rotation([])) == card.CARD_EINVAL  # (a table of none would be read behind its end)
     cfg = card.make_cfg(TINY, 256)
     cfg.head_dim = 96
     assert call(cfg=cfg) == card.CARD_EINVAL
@@ -70,6 +71,23 @@ def test_attend4_and_read_refusals():
     assert read(_batch(n_rows=0)) == card.CARD_OK
     assert read(k=None) == read(v=None) == read(k=_rows(head=0)) == read(v=_rows(row=32)) == read(k=_rows(type=card.CARD_F32)) == card.CARD_EINVAL
     assert read(layer=-1) == card.CARD_ERANGE and read(_batch(k_pages=None)) == card.CARD_EINVAL
+
+
+def test_page_and_slot_lists_of_4_bits():
+    cfg = card.make_cfg(TINY, 256)
+    kv = lambda n_pages=16, k=A, v=A: card.CardKV(k, v, None, n_pages, -1)  # noqa: E731
+    copy = lambda src, dst, kv=kv(): card.card_kv4_copy_pages(cfg, kv, src, dst)  # noqa: E731
+    move = lambda src, dst, kv=kv(): card.card_kv4_move_slots(cfg, kv, src, dst)  # noqa: E731
+    for call, most in ((copy, 16), (move, 256)):
+        assert call([], []) == card.CARD_OK
+        for bad in (-1, most, 2 ** 31 - 1):
+            assert call([bad], [3]) == call([3], [bad]) == card.CARD_ERANGE
+        assert call([1, 2], [9, 9]) == call([1, 9], [9, 10]) == card.CARD_EINVAL  # written twice; read after it was written
+        assert call([0], [1], kv(k=None)) == call([0], [1], kv(v=None)) == call([0], [1], kv(v=A + 8)) == call([0], [1], kv(0)) == card.CARD_EINVAL
+        assert call([1], [2, 3]) == card.CARD_EINVAL
+    assert copy([0, 5], [5, 6]) == copy([5, 0], [6, 5]) == copy([4], [4]) == card.CARD_EINVAL  # read and written
+    for name in ("card_kv4_copy_pages", "card_kv4_move_slots"):
+        assert getattr(card.lib, name)(cfg, kv(), 1, None, None, None) == getattr(card.lib, name)(cfg, kv(), -1, None, None, None) == card.CARD_EINVAL
 
 
 def test_pool_bytes():
