@@ -170,34 +170,3 @@ def test_rows_as_they_lie():
             got = card.beam_select(x, scores.cuda(), 3)
             want, _ = reference(x.cpu(), scores, 3)
             assert torch.equal(got["tokens"].cpu().long(), want["tokens"]) and torch.equal(got["parents"].cpu().long(), want["parents"])
-
-
-def test_beams_in_a_captured_graph():
-    """Replays with other logits, scores and lengths in the same buffers, each against the eager call."""
-    import paper_2508_04462_amd as card
-
-    g = torch.Generator().manual_seed(2)
-    groups, beams, vocab, most = 4, 5, 30011, 64
-    logits, scores = _logits(groups * beams, vocab, F32, 1).cuda(), torch.zeros(groups, beams).cuda()
-    done, history, lengths = (torch.zeros(s, dtype=torch.int32).cuda() for s in ((groups, beams), (groups, beams, most), (groups,)))
-    args = dict(done=done, eos=3, history=history, lengths=lengths)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        card.beam_select(logits, scores, **args)
-    torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        out = card.beam_select(logits, scores, **args)
-    for i in range(4):
-        logits.copy_(_logits(groups * beams, vocab, F32, 10 + i))
-        scores.copy_(-torch.rand((groups, beams), generator=g))
-        done.copy_((torch.rand((groups, beams), generator=g) < 0.3).int())
-        lengths.fill_(i)
-        graph.replay()
-        torch.cuda.synchronize()
-        want = card.beam_select(logits, scores, **args)
-        torch.cuda.synchronize()
-        for name in ("scores", "tokens", "parents", "done"):
-            assert torch.equal(out[name], want[name]), (i, name)
-        assert torch.equal(out["history"][:, :, :i + 1], want["history"][:, :, :i + 1])

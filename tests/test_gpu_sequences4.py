@@ -7,6 +7,7 @@ import torch
 
 import card_inputs as ci
 from cache4_common import model_freqs, quantised, rotated, values
+from test_gpu_beams import _logits as beam_logits
 
 pytestmark = pytest.mark.gpu
 
@@ -249,6 +250,7 @@ def test_append_refuses(monkeypatch):
 def test_operators_in_a_captured_graph():
     """A decoding step of two layers with everything in a graph; between replays other contents, lengths and positions come into its buffers, and eager work runs."""
     import paper_2508_04462_amd as card
+    from paper_2508_04462_amd.runtime import _lane_streams
 
     g = torch.Generator(device="cuda").manual_seed(1)
     pool = card.SequencePool(TOY, 80, 256, bits=4)
@@ -275,13 +277,13 @@ def test_operators_in_a_captured_graph():
         assert st == card.CARD_OK
         return outs, [t.clone() for t in held]
 
-    side = torch.cuda.Stream()
+    side = _lane_streams(torch.device("cuda:0"), 2)[0]  # (of the library's own: with more streams, two of a loop may share a hardware queue)
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         step()
     torch.cuda.current_stream().wait_stream(side)
     graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
+    with torch.cuda.graph(graph, stream=side):
         got = step()
     full = plan.ctx_lens.clone()
     for i in range(4):
@@ -302,9 +304,42 @@ def test_operators_in_a_captured_graph():
         assert torch.equal(after[0], pool.k_pages) and torch.equal(after[1], pool.v_pages)
 
 
+def test_beams_in_a_captured_graph():
+    """Replays with other logits, scores and lengths in the same buffers, each against the eager call."""
+    import paper_2508_04462_amd as card
+    from paper_2508_04462_amd.runtime import _lane_streams
+
+    g = torch.Generator().manual_seed(2)
+    groups, beams, vocab, most = 4, 5, 30011, 64
+    logits, scores = beam_logits(groups * beams, vocab, torch.float32, 1).cuda(), torch.zeros(groups, beams).cuda()
+    done, history, lengths = (torch.zeros(s, dtype=torch.int32).cuda() for s in ((groups, beams), (groups, beams, most), (groups,)))
+    args = dict(done=done, eos=3, history=history, lengths=lengths)
+    side = _lane_streams(torch.device("cuda:0"), 2)[0]  # (of the library's own: with more streams, two of a loop may share a hardware queue)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        card.beam_select(logits, scores, **args)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = card.beam_select(logits, scores, **args)
+    for i in range(4):
+        logits.copy_(beam_logits(groups * beams, vocab, torch.float32, 10 + i))
+        scores.copy_(-torch.rand((groups, beams), generator=g))
+        done.copy_((torch.rand((groups, beams), generator=g) < 0.3).int())
+        lengths.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = card.beam_select(logits, scores, **args)
+        torch.cuda.synchronize()
+        for name in ("scores", "tokens", "parents", "done"):
+            assert torch.equal(out[name], want[name]), (i, name)
+        assert torch.equal(out["history"][:, :, :i + 1], want["history"][:, :, :i + 1])
+
+
 def test_calls_on_another_stream():
     """A plan that is dropped while another stream still works on it; results as on its own stream."""
     import paper_2508_04462_amd as card
+    from paper_2508_04462_amd.runtime import _lane_streams
 
     g = torch.Generator(device="cuda").manual_seed(4)
     pool = card.SequencePool(TOY, 80, 1024, bits=4)
@@ -315,7 +350,7 @@ def test_calls_on_another_stream():
     plan = pool.plan([a], [900])
     want = pool.attend(plan, 0, pool.append(plan, 0, q, k, v), None, None)
     torch.cuda.synchronize()
-    side = torch.cuda.Stream()
+    side = _lane_streams(torch.device("cuda:0"), 2)[0]
     for _ in range(3):
         plan = pool.plan([a], [900])
         side.wait_stream(torch.cuda.current_stream())
