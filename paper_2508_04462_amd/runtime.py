@@ -360,8 +360,9 @@ class Target:
     def beam_search(self, pool, tokens: Sequence[int], beams: int, n_tokens: int, eos: int = -1, temperature: float = 1.0) -> Dict:
         """The `beams` texts behind a prompt that a beam search of n_tokens steps finds: "tokens", a list of each (its last token eos where it has
         ended), and "scores", sums of ln softmax(logits / temperature), best first.  The beams are sequences of `pool` (a SequencePool of the Target's
-        layers and heads), which share the prompt's pages and those of common beginnings; an ended one is not forwarded any more.  CARD_ECAPACITY where the pool or max_ctx has
-        no room; the sequences are freed at the end, and the Target is on what it was attached to."""
+        layers and heads), which share the prompt's pages and those of common beginnings; an ended one is not forwarded any more, and neither it nor any beam
+        after the last step holds pages.  CARD_ECAPACITY where the pool or max_ctx has no room; the sequences are freed at the end, and the Target is on what it was attached
+        to."""
         from .sequences import beam_select
 
         n = len(tokens)
@@ -375,7 +376,7 @@ class Target:
         lengths = torch.zeros(1, dtype=torch.int32, device=dev)
         cand = torch.tensor([int(tokens[-1])], dtype=torch.int32, device=dev)
         done, history = None, torch.zeros((1, 1, n_tokens), dtype=torch.int32, device=dev)
-        ended = [0]
+        live = [0]  # the beams that are forwarded: seqs[i] is that of beam live[i]
         try:
             pool.extend(seqs[0], n)
             self.attach(pool, seqs[0])
@@ -383,24 +384,23 @@ class Target:
                 self.prefill(tokens[:-1])
                 failed = torch.minimum(failed, self.out[0])
             for step in range(n_tokens):
-                for i, seq in enumerate(seqs):
-                    if not ended[i]:
-                        self.attach(pool, seq)
-                        _check(self.enqueue_verify(n - 1 + step, -1, 1, logits[i:i + 1], cand=cand[i:i + 1]), "card_verify")
-                        failed = torch.minimum(failed, self.out[0])
-                got = beam_select(logits[:len(seqs)], scores, beams, done, eos, temperature, history, lengths)
+                for i, seq in zip(live, seqs):
+                    self.attach(pool, seq)
+                    _check(self.enqueue_verify(n - 1 + step, -1, 1, logits[i:i + 1], cand=cand[i:i + 1]), "card_verify")
+                    failed = torch.minimum(failed, self.out[0])
+                got = beam_select(logits[:scores.shape[1]], scores, beams, done, eos, temperature, history, lengths)
                 scores, done, history, cand = got["scores"], got["done"], got["history"], got["tokens"][0]
                 lengths = lengths + 1
                 *said, status = torch.cat([got["parents"][0], done[0], failed.view(1)]).tolist()
                 if status < 0:  # weights not packed
                     raise B.CardError(B.CARD_EDEVICE, "beam_search")
-                ended = said[beams:]
-                seqs = pool.reorder(seqs, said[:beams])
-                if all(ended) or step + 1 == n_tokens:
+                goes_on = [i for i in range(beams) if not said[beams + i]]
+                if not goes_on or step + 1 == n_tokens:
                     break
-                for i, seq in enumerate(seqs):
-                    if not ended[i]:
-                        pool.extend(seq, 1)
+                seqs = pool.reorder(seqs, [live.index(said[i]) for i in goes_on])  # (the parent of one that goes on was forwarded)
+                live = goes_on
+                for seq in seqs:
+                    pool.extend(seq, 1)
         finally:
             self._attached = before
             for seq in seqs:
