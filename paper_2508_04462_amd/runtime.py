@@ -369,14 +369,13 @@ class Target:
         if n < 1 or beams < 1 or n_tokens < 1 or min(tokens) < 0 or max(tokens) >= self.cfg.vocab:
             raise B.CardError(B.CARD_ERANGE, "beam_search")
         before, dev = self._attached, self.device
-        seqs = [pool.new()]
         failed = torch.zeros((), dtype=torch.int32, device=dev)
         logits = torch.empty((beams, self.cfg.vocab), dtype=torch.float32, device=dev)
         scores = torch.zeros((1, 1), dtype=torch.float32, device=dev)
         lengths = torch.zeros(1, dtype=torch.int32, device=dev)
         cand = torch.tensor([int(tokens[-1])], dtype=torch.int32, device=dev)
         done, history = None, torch.zeros((1, 1, n_tokens), dtype=torch.int32, device=dev)
-        live = [0]  # the beams that are forwarded: seqs[i] is that of beam live[i]
+        seqs, live = [pool.new()], [0]  # of the beams that are forwarded: seqs[i] is that of beam live[i]
         try:
             pool.extend(seqs[0], n)
             self.attach(pool, seqs[0])

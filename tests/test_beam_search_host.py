@@ -104,3 +104,11 @@ def test_search_without_room(monkeypatch):
     with pytest.raises(card.CardError) as e:
         target.beam_search(pool, list(range(20)), 4, 2)
     assert e.value.status == card.CARD_ECAPACITY and pool.free_pages == 3 and not pool._seqs and target._attached is None
+
+
+def test_search_whose_buffers_find_no_room(monkeypatch):
+    """Nothing of the call stays in the caller's pool."""
+    target, pool = PlayedTarget(monkeypatch, vocab=1 << 60), PlayedPool(monkeypatch, 3, 512)
+    with pytest.raises(RuntimeError):
+        target.beam_search(pool, list(range(20)), 4, 2)
+    assert not pool._seqs and pool.free_pages == 3
