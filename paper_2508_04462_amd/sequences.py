@@ -173,7 +173,7 @@ class SequencePool:
             slot = lambda p: s.pages[p // 16] * 16 + p % 16  # noqa: E731
             with torch.cuda.device_of(self.k_pages):
                 move = B.card_kv_move_slots if self.bits == 16 else B.card_kv4_move_slots
-                _check(move(self.cfg, self.kv(seq), [slot(p) for p, _ in moves], [slot(q) for _, q in moves], self._stream()), "card_kv_move_slots")
+                _check(move(self.cfg, self._pools(), [slot(p) for p, _ in moves], [slot(q) for _, q in moves], self._stream()), "card_kv_move_slots")
         self.truncate(seq, first + len(pos))
 
     def reorder(self, seqs: Sequence[int], parents: Sequence[int]) -> List[int]:
@@ -227,7 +227,9 @@ class SequencePool:
 
     # -- device side
     def kv(self, seq: int, pending: int = -1) -> B.CardKV:
-        """The sequence as steps, prompts and card_kv_gather take it."""
+        """The sequence as steps, prompts and card_kv_gather take it, of a pool of 16 bits: they would read far behind the end of one of 4."""
+        if self.bits != 16:
+            raise ValueError("a pool of 4 bits: steps, prompts and card_kv_gather take 16")
         return B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), self._seqs[seq].table.data_ptr(), self.n_pages, int(pending))
 
     def plan(self, seqs: Sequence[int], new: Sequence[int]) -> AttendPlan:
@@ -352,11 +354,13 @@ class SequencePool:
             s.pages[i] = d
         self._upload(s)
 
+    def _pools(self) -> B.CardKV:
+        return B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), None, self.n_pages, -1)
+
     def _copy_pages(self, src: Sequence[int], dst: Sequence[int]) -> None:
-        kv = B.CardKV(self.k_pages.data_ptr(), self.v_pages.data_ptr(), None, self.n_pages, -1)
         with torch.cuda.device_of(self.k_pages):
             copy = B.card_kv_copy_pages if self.bits == 16 else B.card_kv4_copy_pages
-            _check(copy(self.cfg, kv, src, dst, self._stream()), "card_kv_copy_pages")
+            _check(copy(self.cfg, self._pools(), src, dst, self._stream()), "card_kv_copy_pages")
 
     def _upload(self, s: _Sequence) -> None:
         s.table[:len(s.pages)] = torch.tensor(s.pages, dtype=torch.int32, device=self.device)
