@@ -608,8 +608,9 @@ int card_logprobs(const void* logits_dev, int32_t type, int32_t rows, int32_t vo
                   int32_t* top_tokens_dev, float* top_logprobs_dev, void* workspace_dev, void* stream);
 
 /* Beam search, one step: of each of `groups` searches, the out_beams best continuations of its beams.  A candidate is a beam and a token of the vocabulary, its score the beam's
- * score + ln softmax(logits / temperature) of the token; a beam that has ended has one candidate, itself, with its score and eos_token.  Candidates are
- * compared in 64 bits; equal scores go by beam, then by token.  Row group * beams + beam of logits_dev belongs to a beam; those of beams that have ended are not
+ * score + ln softmax(logits / temperature) of the token; a beam that has ended has one candidate, itself, with its score and eos_token.  Candidates of one
+ * beam are in the order of their logits, equal ones by token; those of different beams are compared by their scores in 64 bits, equal ones by beam.  (The softmax's
+ * sum is one of 32 bits: ln of it is certain to some 1e-6, and the same wherever a row of the same logits lies.)  Row group * beams + beam of logits_dev belongs to a beam; those of beams that have ended are not
  * read.  The histories of the beams move with them: out_history of a new beam is that of its parent, lengths[group] tokens, and then its token
  * (where there is room for it; what lies behind is not touched).
  *   logits_dev, type, vocab, row_stride, temperature: as card_logprobs

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kLpThreads) void k_beam_rows(BeamArgs b) {
     __shared__ LogprobShared sm;
     const int row = blockIdx.x, part = blockIdx.y;
     if (b.done && b.done[row] != 0) return;
-    const RowSums r = scan_part<T, false>(b.rows, sm, row, part);
+    const RowSums r = scan_part<T, false, true>(b.rows, sm, row, part);
     leave_part(b.rows, sm, r, row, part);
 }
 
