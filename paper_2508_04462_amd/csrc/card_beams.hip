@@ -39,9 +39,9 @@ __global__ __launch_bounds__(kLpThreads) void k_beam_rows(BeamArgs b) {
 }
 
 __device__ __forceinline__ float first_lane(float v) { return __uint_as_float(uint32_t(__builtin_amdgcn_readfirstlane(int(__float_as_uint(v))))); }
-// Scores as numbers in the same order; 0: none.
+// Scores as numbers in the same order (-0 as 0); 0: none.
 __device__ __forceinline__ unsigned long long score_key(double s) {
-    const unsigned long long u = __builtin_bit_cast(unsigned long long, s);
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, s + 0.0);
     return s > -INFINITY ? (u >> 63 ? ~u : u | 1ull << 63) : 0ull;
 }
 __device__ __forceinline__ unsigned long long max_of_lanes(unsigned long long v) {

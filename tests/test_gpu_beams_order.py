@@ -45,3 +45,16 @@ def test_the_same_logits_at_other_addresses(vocab, dtype):
             got = card.beam_select(wide.cuda()[:, first:first + vocab], scores, 4)
             for name in want:
                 assert torch.equal(got[name], want[name]), (first, stride, name)
+
+
+def test_zero_and_minus_zero_are_equal_scores():
+    import paper_2508_04462_amd as card
+
+    x = torch.full((2, 300), -float("inf"))
+    x[:, 200] = 5.0  # probability 1
+    for scores, done in (([-0.0, 0.0], [1, 0]), ([0.0, -0.0], [0, 1])):
+        got = card.beam_select(x.cuda(), torch.tensor([scores]).cuda(), 2, done=torch.tensor([done], dtype=torch.int32).cuda(), eos=4)
+        assert got["parents"][0].tolist() == [0, 1], scores
+        # (more candidates: they are taken one by one)
+        got = card.beam_select(x.repeat(16, 1).cuda(), torch.tensor([scores * 16]).cuda(), 32, done=torch.tensor([done * 16], dtype=torch.int32).cuda(), eos=4)
+        assert got["parents"][0].tolist() == list(range(32)), scores
