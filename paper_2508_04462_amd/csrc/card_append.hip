@@ -134,10 +134,12 @@ __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
     for (int i = 0; i < 2; ++i) reinterpret_cast<floatx4*>(p)[i] = floatx4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
 }
 
-// The rows of one page of a sequence: token t of the page, t0 <= t < t1, is row row0 + t.  Those below `stored` have a place in the sequence's table.
+// The rows of one page of a sequence: token t of the page, t0 <= t < t1, is row row0 + t, at position place0 + t.  Those below `stored` have a place in the sequence's table.
+// (Places are counted from the table's end for a sequence that is longer than that; positions are not.)
 struct PageRows {
     int32_t slot0, t0, t1, stored, page;
     int64_t row0;
+    double place0;
     bool some;
 };
 __device__ __forceinline__ PageRows rows_of_page(const AttendArgs& a, int unit) {
@@ -149,6 +151,7 @@ __device__ __forceinline__ PageRows rows_of_page(const AttendArgs& a, int unit) 
     r.t0 = max(u.ctx - r.slot0, 0);
     r.t1 = min(end - r.slot0, 16);
     r.row0 = int64_t(u.row0) + r.slot0 - u.ctx;
+    r.place0 = double(u.held) + (r.slot0 - u.ctx);
     r.stored = 0;
     r.page = -1;
     if (r.some && pg < a.table_pages) {
@@ -194,9 +197,9 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs g) {
     if (g.rotate) {
         for (int e = tid; e < n * (H / 2); e += 256) {
             const int t = r.t0 + e / (H / 2), j = e % (H / 2);
-            const int position = g.positions ? g.positions[r.row0 + t] : r.slot0 + t;
+            const double position = g.positions ? double(g.positions[r.row0 + t]) : r.place0 + t;
             float2 cs;
-            cos_sin(double(position) * g.turns[j], cs.x, cs.y);
+            cos_sin(position * g.turns[j], cs.x, cs.y);
             table[t][j] = cs;
         }
         __syncthreads();

@@ -36,6 +36,7 @@ __device__ __forceinline__ uint32_t bf16_bits(__bf16 v) { return __builtin_bit_c
 // sequence s has the units from floor(start_s * mul / div) + add * s on, which are enough for ceil(new_s * mul / div) + add - 1 of them.
 struct SeqUnit {
     int32_t seq, index, row0, n_new, ctx, len;
+    int32_t held;  // tokens in the cache as the lengths say it; ctx: as far as the table goes
 };
 __device__ __forceinline__ int32_t seq_start(const AttendArgs& a, int s) {
     return min(max(a.starts[s], 0), a.n_rows);
@@ -60,7 +61,8 @@ __device__ __forceinline__ SeqUnit find_unit(const AttendArgs& a, int unit, int 
     u.index = unit - first(u.row0, u.seq);
     u.n_new = max(__builtin_amdgcn_readlane(end, at) - u.row0, 0);
     const int room = a.table_pages * 16;
-    u.ctx = min(max(__builtin_amdgcn_readlane(held, at), 0), room);
+    u.held = max(__builtin_amdgcn_readlane(held, at), 0);
+    u.ctx = min(u.held, room);
     u.len = min(u.ctx + u.n_new, room);
     return u;
 }
