@@ -494,7 +494,7 @@ typedef struct card_kv_batch {
     int32_t n_pages;
     int32_t n_seqs;
     const int32_t* block_tables; /* dev [n_seqs][table_pages], entries in [0, n_pages) as far as the sequence reaches */
-    int32_t table_pages;
+    int32_t table_pages;       /* less than 2^27 - 2^24                                        */
     int32_t n_rows;            /* rows of the arrays of the call                                 */
     const int32_t* ctx_lens;   /* dev [n_seqs]                                                   */
     const int32_t* row_starts; /* dev [n_seqs + 1], ascending from 0, the last one at most n_rows */

@@ -145,7 +145,7 @@ struct PageRows {
 __device__ __forceinline__ PageRows rows_of_page(const AttendArgs& a, int unit) {
     const SeqUnit u = find_unit(a, unit, 1, 16, kStoreUnits);
     PageRows r;
-    const int pg = (u.ctx >> 4) + u.index, end = min(u.ctx, 0x7fffffff - u.n_new) + u.n_new;
+    const int pg = (u.ctx >> 4) + u.index, end = u.ctx + u.n_new;
     r.slot0 = pg * 16;
     r.some = u.index >= 0 && r.slot0 < end && u.n_new > 0;
     r.t0 = max(u.ctx - r.slot0, 0);

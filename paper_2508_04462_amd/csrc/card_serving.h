@@ -21,13 +21,15 @@ inline bool rows_ok(const card_rows* r, int32_t type, int64_t least_stride) {
            r->row_stride % unit == 0 && r->head_stride % unit == 0;
 }
 
-inline bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
-    return cfg_valid(cfg) && b && b->n_pages > 0 && b->n_seqs > 0 && b->table_pages > 0 && b->table_pages < (1 << 27) && b->n_rows >= 0 &&
-           b->max_new >= 0 && b->max_len >= 0;
-}
-
 // A launch has less than 2^32 threads in x: 2^24 workgroups of 256.  (units of 16 rows x heads, and of 16 new tokens)
 constexpr int64_t kMostGroups = int64_t(1) << 24;
+// The kernels count places of a sequence in 32 bits: those of its table and behind them the 16 of each unit that a launch may have (and with them all new tokens, fewer
+// than 2^28).
+constexpr int32_t kMostTablePages = (1 << 27) - (1 << 24) - 1;
+inline bool batch_ok(const card_model_cfg* cfg, const card_kv_batch* b) {
+    return cfg_valid(cfg) && b && b->n_pages > 0 && b->n_seqs > 0 && b->table_pages > 0 && b->table_pages <= kMostTablePages && b->n_rows >= 0 &&
+           b->max_new >= 0 && b->max_len >= 0;
+}
 inline bool batch_fits(const card_model_cfg* cfg, const card_kv_batch* b) {
     return int64_t(b->n_rows) * cfg->n_q_heads / 16 + int64_t(kStoreUnits) * b->n_seqs * cfg->n_kv_heads < kMostGroups;
 }

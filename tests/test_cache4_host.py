@@ -115,3 +115,17 @@ def test_definition_of_4_bits():
         assert ((values(codes, words) - x.double()).abs() <= scale * (0.5 + 2.0 ** -16)).all()
     b = Batch((4, 2, 64), [(3, 2)], torch.float32)
     assert b.n_rows == 2
+
+
+def test_longest_tables():
+    """Places are counted in 32 bits: of a table and of all new tokens that a launch has room for behind it."""
+    cfg = card.make_cfg(TINY, 256)
+    limit = (1 << 27) - (1 << 24)
+    calls = [lambda b, name=name: _append(name, batch=b) for name in ("card_kv_append", "card_kv4_append")]
+    calls += [lambda b, name=name: getattr(card, name)(cfg, b, 0, _rows(), None, None, _rows(), None, A) for name in ("card_kv_attend", "card_kv4_attend")]
+    calls += [lambda b: card.card_kv4_read(cfg, b, 0, _rows(), _rows())]
+    for call in calls:
+        assert call(_batch(table_pages=limit, n_rows=0)) == call(_batch(table_pages=limit)) == card.CARD_EINVAL
+        assert call(_batch(table_pages=limit - 1, n_rows=0)) == card.CARD_OK
+    # page and place of the last unit of the largest launch, and the end of all its new tokens
+    assert ((limit - 1) + (1 << 24)) * 16 + 15 < 1 << 31 and (limit - 1) * 16 + (1 << 28) < 1 << 31
