@@ -161,7 +161,9 @@ __global__ __launch_bounds__(256, NT * sizeof(T) == 2 ? 3 : 2) void k_attend4(At
     constexpr int ST = H / 32, HT = H / 16, NP = sizeof(T) == 4 ? 3 : 1, NW = kWeightParts<T>, LD = H + 4, CH = H / 16, G = H / 64, ROUND = 2;
     constexpr bool FINE = sizeof(T) == 4;
     using P4 = Page4<H>;
-    __shared__ float red[4][16][LD], red_m[4][16], red_l[4][16];
+    __shared__ __align__(16) float red[4][16][LD];  // (written as floatx4)
+    __shared__ float red_m[4][16], red_l[4][16];
+    static_assert(__alignof__(red) % 16 == 0 && LD % 4 == 0, "");
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kq = lane >> 4, cut = blockIdx.y;
     const int kvh = blockIdx.x % uint32_t(a.Hkv), at_unit = blockIdx.x / uint32_t(a.Hkv);
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
