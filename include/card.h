@@ -547,8 +547,8 @@ int card_kv_attend(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
  *   q, q_out : n_q_heads heads, or both NULL where queries are not rotated; q_out may be q, or overlaps no array of the call.  Strides of
  *              q_out at least head_dim
  *   k, v     : n_kv_heads heads; they are not changed.  All of one type, CARD_BF16 or CARD_F32, data and strides in multiples of 16 bytes
- * Angles are made in 64 bits and products added in 64: what is stored or put out is the exact value rounded to its type, from
- * cosines and sines rounded to fp32.  Rows behind row_starts[n_seqs] are not touched; tokens whose page is outside the pool or the table are not stored,
+ * Angles, cosines and sines are made in 64 bits, an angle off by 2^-50 of itself at most, and rounded to fp32; products are added in 64 bits, and the sum is rounded to fp32 and then
+ * to its type.  Positions that are not given count from ctx_lens, whatever the table holds.  Rows behind row_starts[n_seqs] are not touched; tokens whose page is outside the pool or the table are not stored,
  * their queries are rotated all the same.  Only the slots of new tokens are written (a pool that steps and prompts run on too: card_kv_attend).
  * Errors: CARD_EINVAL (also for frequencies that are not finite), CARD_ERANGE (as card_kv_attend), CARD_EDEVICE; nothing is enqueued on error. */
 typedef struct card_rotation {
@@ -570,7 +570,7 @@ int card_kv_append(const card_model_cfg* cfg, const card_kv_batch* batch, int32_
  * ((l * n_pages + p) * n_kv_heads + a) * 9 * head_dim.  Steps, prompts, drafts and the functions above take pools of 16 bits only, those
  * here pools of 4 only.  The pools need no initialisation.
  *
- * card_kv4_append  : card_kv_append; rotated keys go to their codes unrounded.
+ * card_kv4_append  : card_kv_append; rotated keys go to their codes as they are in fp32.
  * card_kv4_read    : what the cache holds of the rows of a batch: k and v [rows][n_kv_heads], strides at least head_dim.  Rows of tokens
  *                    without a page are not touched.
  * card_kv4_attend  : card_kv_attend over the values that the codes stand for.  Codes enter the products exactly; what a row does not see may hold anything, also

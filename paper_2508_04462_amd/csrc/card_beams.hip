@@ -2,8 +2,9 @@
 //
 // A candidate's score is its beam's score + (x - m) / T - ln s, with m the beam's largest logit and s = sum e^((x - m) / T): inside a beam the order of scores is that of the
 // logits, so of each beam only its most probable tokens matter, as many as there are beams to go on with.  One pass over the logits finds them with m and s
-// (scan_part): 40 searches of 6 beams, 152064 tokens in bf16, 73 MB, in 23 us, then 7.7 to join them; a search of 4 of 128256 in fp32
-// 5.8 + 6.4.  The large ones are bound by the instructions of a logit (an exponential and some eight more), the small ones by latency.  Scores of several beams are compared in 64 bits, so that sums of hundreds of log probabilities do not hide what
+// (scan_part): 40 searches of 6 beams, 152064 tokens in bf16, an eighth of the beams ended, so 64 MB, in 23.2 us (2.8 TB/s), then 7.7 to join them; a search of 4 of 128256 in fp32
+// 5.7 + 6.8.  The first is short rather than bound by one thing: 840 workgroups, one wave of them, vector units busy 43 % of the time (an exponential and some eight more instructions a
+// logit), wavefronts waiting 58 %; 1000 rows go through the same pass at 5.2 TB/s.  The small ones are bound by latency.  Scores of several beams are compared in 64 bits, so that sums of hundreds of log probabilities do not hide what
 // the candidates differ by.
 #pragma once
 #include "card_logprobs.hip"

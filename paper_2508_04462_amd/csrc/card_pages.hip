@@ -130,8 +130,9 @@ __global__ __launch_bounds__(H / 64 * 192) void k_kv_move_slots(MoveArgs a) {
 }
 
 // The same in pages of 4 bits a value (Page4).  One workgroup: one head of one layer, a wavefront for K and one for V; sixteen lanes have a token, a lane the words or bytes of its
-// channels for all moves, and all of a round is read before any is written, which is the order of the list, as above.  1500 tokens of 32 layers x 8 heads x 128 152 us (a token after the other
-// 700), 128 13, 32 6.5.  157 pages are copied by k_kv_copy_pages in 23 us.
+// channels for all moves, and all of a round is read before any is written, which is the order of the list, as above.  1500 tokens of 32 layers x 8 heads x 128, 110 MB, 152 us (a token after the other
+// 700), 128 13, 32 6.2: more than the 122 of 16 bits with 3.5 times the bytes, by latency: two wavefronts of a head and layer instead of six, and a round is read only when the one before it is
+// written.  157 pages are copied by k_kv_copy_pages in 23 us.
 constexpr int kMoveRound4 = 24;  // tokens of a lane: four times as many in a round
 template <int H>
 __global__ __launch_bounds__(128) void k_kv4_move_slots(MoveArgs a) {
